@@ -391,6 +391,30 @@ gkv_status gkv_rd_residual_select(gkv_cache *c, const uint16_t *k_src, const uin
                                   const float *mass, int32_t nkeep, void *ws, int64_t ws_bytes,
                                   void *stream);
 
+/* ---------------------------------------------------------------- many queries */
+
+/* Causal attention over packed prompts of different lengths, before anything is graded:
+ * for prompt b of len_host[b] tokens (packed one after the other), query head g of its
+ * token i reads keys and values 0 .. i of KV head g / G of the same prompt,
+ *   out[i][g][:] = sum_{j <= i} softmax_j(q_ig . k_j / sqrt(128)) v_j.
+ * dtype: GKV_F16 or GKV_BF16, the type of q, k, v and out.  q, out: rows of [Hq][128] at
+ * q_stride / out_stride elements from token to token; k, v: rows of [Hkv][128] at k_stride /
+ * v_stride (so q, k and v may be slices of one projection's output).  Pointers are 16-byte
+ * aligned and strides multiples of 8 elements (GKV_E_ARG), a stride is at least its row
+ * (GKV_E_SHAPE) and at most GKV_MAX_ROW_STRIDE (GKV_E_UNSUPPORTED).  Lengths may be 0 (the
+ * prompt has no rows).  out must not overlap the inputs.  Logits, maxima and sums are
+ * fp32; probabilities enter the value product, and outputs are stored, rounded to the
+ * type.  A token that a row does not see has no effect on it, whatever its key and value
+ * hold (infinities and NaN included).  GKV_E_UNSUPPORTED for more than GKV_MAX_PROMPTS
+ * prompts or GKV_MAX_PROMPT_TOKENS tokens in one call. */
+typedef enum gkv_dtype { GKV_F16 = 0, GKV_BF16 = 1 } gkv_dtype;
+#define GKV_MAX_PROMPTS 256
+#define GKV_MAX_PROMPT_TOKENS 100000000
+#define GKV_MAX_ROW_STRIDE 1048576
+gkv_status gkv_prompt_attn(const void *q, const void *k, const void *v, void *out, int32_t dtype, int32_t Hkv,
+                           int32_t Hq, int32_t nseq, const int64_t *len_host, int64_t q_stride, int64_t k_stride,
+                           int64_t v_stride, int64_t out_stride, void *stream);
+
 /* ---------------------------------------------------------------- multi-layer service */
 
 /* One decode step of cache maintenance for L layers (section 3.2: incremental append

@@ -95,6 +95,7 @@ _observe = _sig("gkv_observe_mass", _i32,
 _query_norms = _sig("gkv_query_norms", _i32, [_vp, _i32, _i32, _i32, _i32, _vp, _vp])
 _allocate = _sig("gkv_allocate_levels", _i32,
                  [_vp, _vp, _vp, _i32, _i32, _i64, ctypes.c_double, ctypes.c_double, _i32, _i32, _vp, _vp])
+_prompt_attn = _sig("gkv_prompt_attn", _i32, [_vp] * 4 + [_i32] * 4 + [_vp] + [_i64] * 4 + [_vp])
 ROUNDING = {"up": 0, "nearest": 1}
 
 EXPORTED = [
@@ -105,7 +106,7 @@ EXPORTED = [
     "gkv_attn_plan", "gkv_attn_partials", "gkv_attn_merge", "gkv_graded_decode_attn_bound",
     "gkv_observe_ws_bytes", "gkv_observe_mass", "gkv_query_norms", "gkv_allocate_levels", "gkv_layers_step",
     "gkv_cache_changed", "gkv_graded_decode_attn_noalloc", "gkv_noalloc_scratch_bytes", "gkv_retire_sequence",
-    "gkv_admit_sequence", "gkv_stream_read_probe",
+    "gkv_admit_sequence", "gkv_stream_read_probe", "gkv_prompt_attn",
 ]
 
 
@@ -201,6 +202,55 @@ def allocate_levels(k, mass, qn, c, tau, window, rounding="up"):
     _check(_allocate(_dptr(k), _dptr(mass), _dptr(qn), B, Hkv, T, float(c), float(tau), int(window),
                      ROUNDING[rounding], _dptr(lv), _stream()), "allocate_levels")
     return lv
+
+
+def _rows_dev(x, what, device=None):
+    """Token rows [n][heads][128] on the device: fp16 or bf16, or fp16 bit patterns.  A view
+    whose heads lie side by side in 16-byte aligned rows is taken as it is, any other one is
+    copied."""
+    if isinstance(x, np.ndarray):
+        x = torch.from_numpy(np.ascontiguousarray(x).view(np.int16))
+    if x.dtype == torch.int16:
+        x = x.view(torch.float16)
+    if x.dtype not in (torch.float16, torch.bfloat16) or x.dim() != 3 or x.shape[2] != D:
+        raise GkvError(-2, what)
+    if device is not None and x.device != device or not x.is_cuda:
+        x = x.to(device if device is not None else "cuda")
+    if x.shape[0] and (x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != D) or x.data_ptr() % 16 or
+                       (x.shape[0] > 1 and (x.stride(0) % 8 or x.stride(0) < x.shape[1] * D))):
+        x = x.contiguous()
+        if x.data_ptr() % 16:  # a contiguous view that starts inside a 16-byte unit
+            x = x.clone()
+    return x
+
+
+def _row_stride(x):
+    """Elements from one token's rows to the next one's."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * D
+
+
+def prompt_attn(q, k, v, lens, out=None):
+    """gkv_prompt_attn: causal attention over packed prompts of lens tokens.  q [n][Hq][128],
+    k, v [n][Hkv][128] (n = sum of lens), all fp16 (or its bits) or all bf16; views with a
+    token stride are read in place.  Returns out [n][Hq][128] in the inputs' type."""
+    q = _rows_dev(q, "prompt_attn")
+    k, v = _rows_dev(k, "prompt_attn", q.device), _rows_dev(v, "prompt_attn", q.device)
+    lens = np.ascontiguousarray(lens, dtype=np.int64).reshape(-1)
+    n, Hq, _ = q.shape
+    if k.shape != v.shape or k.shape[0] != n or int(lens.sum()) != n:
+        raise GkvError(-2, "prompt_attn")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise GkvError(-1, "prompt_attn")
+    if out is None:
+        out = torch.empty((n, Hq, D), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or (
+            n and (out.stride(2) != 1 or out.stride(1) != D)):
+        raise GkvError(-2, "prompt_attn")
+    with torch.cuda.device(q.device):
+        _check(_prompt_attn(_dptr(q), _dptr(k), _dptr(v), _dptr(out), int(q.dtype == torch.bfloat16), k.shape[1], Hq,
+                            len(lens), _np_ptr(lens), _row_stride(q), _row_stride(k), _row_stride(v),
+                            _row_stride(out), _stream()), "prompt_attn")
+    return out
 
 
 def stream_read_probe(buf, sink):

@@ -1,0 +1,321 @@
+// Attention of many query rows over tiles of keys and values in LDS: the part that the
+// packed-prompt kernel (prompt.hip) and the chunk kernel (chunk.hip) share.
+//
+// Rows.  The G query heads of a KV head read the same keys, so the rows of one (sequence,
+// KV head) are its (token, head) pairs in one order, row r = token r / G, head r % G: a
+// tile of rows spans few tokens (little of a causal tile is masked away) and one token's
+// heads fill a tile together.  A wavefront holds 32 rows.
+//
+// Arithmetic per 32-token group, on 32x32x16 MFMA (32 cycles each; the 16x16x32 form took
+// 18.4 ns for the same products beside six vector instructions, this one 15.4):
+//   S^T[token][row] = sum_d K[token][d] Q[row][d]          8 instructions
+//   p = 2^(S sl2 - m)   (sl2 = log2(e) / sqrt(128), m per row)
+//   O^T[d][row]    += sum_t V[t][d] p[t][row]              4 x 2 instructions
+// With S transposed, a lane holds one row's scores in the accumulator layout (lane l: row
+// l & 31, tokens 8 (i >> 2) + 4 (l >> 5) + (i & 3)), which is, two values a register, the
+// layout of the second product's operand when its inner index runs over the tokens in that
+// same order: the probabilities never leave their lane.  O^T has a row per lane too, so the
+// rescale by a new maximum is one factor per lane.
+//
+// The running maximum is only raised when some score passes it by more than kRescale
+// (2^8): probabilities stay below 2^8 (far inside fp16), the sums are in fp32 and the
+// common tile has no cross-lane step.  Probabilities enter the second product in the
+// type of the values (one rounding of at most half a step each); the sum of a row adds
+// the rounded ones, so the weights of a row sum to 1 as the product sees them.
+//
+// A masked score becomes -infinity by selection, never by arithmetic, so a NaN or infinity
+// in a masked key has no effect; for masked values see outputs_masked.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gkv {
+namespace ta {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr int kRows = 32;          // rows of a wavefront
+constexpr float kRescale = 8.0f;   // lazy rescale threshold (log2 units)
+
+struct F16 {
+  static constexpr uint32_t kExp = 0x7C007C00u;  // exponent bits of a pair
+  __device__ static f16v mfma(u4 a, u4 b, f16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0,
+                                                  0);
+  }
+  __device__ static uint32_t pack(float x, float y) {
+    half2v h;
+    h[0] = (_Float16)x;
+    h[1] = (_Float16)y;
+    return __builtin_bit_cast(uint32_t, h);
+  }
+  // acc + the two values of p
+  __device__ static float add2(uint32_t p, float acc) {
+    half2v one;
+    one[0] = one[1] = (_Float16)1.0f;
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, p), one, acc, false);
+  }
+  // acc + 0 times each value of p: NaN if one is infinite or NaN
+  __device__ static float times0(uint32_t p, float acc) {
+    half2v none;
+    none[0] = none[1] = (_Float16)0.0f;
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, p), none, acc, false);
+  }
+  __device__ static float widen(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
+};
+struct BF16 {
+  static constexpr uint32_t kExp = 0x7F807F80u;
+  __device__ static f16v mfma(u4 a, u4 b, f16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+  }
+  __device__ static uint32_t pack(float x, float y) {
+    bf2 h;
+    h[0] = (__bf16)x;
+    h[1] = (__bf16)y;
+    return __builtin_bit_cast(uint32_t, h);
+  }
+  __device__ static float add2(uint32_t p, float acc) {
+    bf2 one;
+    one[0] = one[1] = (__bf16)1.0f;
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, p), one, acc, false);
+  }
+  __device__ static float times0(uint32_t p, float acc) {
+    bf2 none;
+    none[0] = none[1] = (__bf16)0.0f;
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, p), none, acc, false);
+  }
+  __device__ static float widen(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
+};
+
+// ---------------------------------------------------------------- LDS tiles
+// Keys: row-major rows of 256 B, 16-byte unit u of row r at place u ^ (r & 15): the 16 rows
+// that a 16-byte read serves at once lie on distinct banks.
+// Values, transposing form (kTr): row-major, unit u of row r at u ^ 4 (r & 3); read with
+// ds_read_b64_tr_b16, which hands each of 16 lanes one column of four rows.
+// Values, operand form: [16-token page][32-channel group][lane] units that hold what the
+// lane feeds the MFMA (tokens 4 (l >> 5) .. + 3 and those + 8 of channel 32 ct + (l & 31)).
+__device__ __forceinline__ uint32_t key_place(int row, int unit) { return row * 256 + ((unit ^ (row & 15)) << 4); }
+__device__ __forceinline__ uint32_t value_place(int row, int unit) {
+  return row * 256 + ((unit ^ ((row & 3) << 2)) << 4);
+}
+
+typedef __attribute__((address_space(3))) const u4 *LdsU4;
+typedef __attribute__((address_space(3))) short4v *LdsTr;
+__device__ __forceinline__ u4 lds_u4(uint32_t at) { return *(LdsU4)(uintptr_t)at; }
+__device__ __forceinline__ u2 lds_tr(uint32_t at) {
+  return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsTr)(uintptr_t)at));
+}
+
+// Lane addresses of the operand reads, relative to a tile's first byte.
+struct Lane {
+  int lane, col, hf;  // lane, row of the wavefront (l & 31), half (l >> 5)
+  uint32_t k0;        // key operand of channels 0..15: the others are k0 ^ (s << 5)
+  uint32_t v0;        // value operand of channel group 0: the others v0 ^ (ct << 6) (kTr), + 1024 ct (operand form)
+  template <bool kTr>
+  __device__ __forceinline__ void init() {
+    lane = threadIdx.x & 63;
+    col = lane & 31;
+    hf = lane >> 5;
+    k0 = key_place(col, hf);
+    if (kTr) {
+      const int r = (lane & 15) >> 2;
+      v0 = value_place(4 * hf + r, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+    } else {
+      v0 = lane * 16;
+    }
+  }
+};
+
+// One wavefront's rows.
+struct Rows {
+  f16v o[4];  // O^T: register i of group ct is channel 32 ct + 8 (i >> 2) + 4 hf + (i & 3)
+  float m;    // what exponents are taken relative to (log2 units, both halves alike)
+  float raise;  // an exponent above this moves m: -infinity while the row has seen nothing
+  float l;    // this half's sum
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+    m = 0.f;
+    raise = -__builtin_inff();
+    l = 0.f;
+  }
+};
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// The value operand of 16-token page kk and channel group ct.
+template <bool kTr>
+__device__ __forceinline__ u4 value_operand(const Lane &ln, uint32_t vbase, int kk, int ct) {
+  if constexpr (kTr) {
+    const uint32_t at = vbase + (ln.v0 ^ (ct << 6)) + kk * 4096;
+    const u2 a = lds_tr(at), b = lds_tr(at + 2048);
+    return u4{a[0], a[1], b[0], b[1]};
+  } else {
+    return lds_u4(vbase + ln.v0 + (kk * 4 + ct) * 1024);
+  }
+}
+
+// Pairs of v with infinity or NaN, as a mask of 16-bit halves.
+template <class T>
+__device__ __forceinline__ uint32_t bad_halves(uint32_t x) {
+  const uint32_t lo = T::kExp & 0xFFFFu;
+  return ((x & lo) == lo ? 0xFFFFu : 0u) | ((x & (lo << 16)) == (lo << 16) ? 0xFFFF0000u : 0u);
+}
+
+// S^T of NT 32-token groups.
+template <class T, int NT>
+__device__ __forceinline__ void scores(f16v (&s)[NT], const Lane &ln, const u4 (&q)[8], uint32_t kbase) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+  for (int d = 0; d < 8; ++d)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s[t] = T::mfma(lds_u4(kbase + (ln.k0 ^ (d << 5)) + t * 8192), q[d], s[t]);
+}
+
+// Scores of tokens whose bit in vis (of this lane's row) is clear become -infinity.
+template <int NT>
+__device__ __forceinline__ void mask_scores(f16v (&s)[NT], const Lane &ln, uint64_t vis) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const uint32_t w = (uint32_t)(vis >> (32 * t)) >> (4 * ln.hf);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      s[t][i] = (w >> (8 * (i >> 2) + (i & 3))) & 1u ? s[t][i] : -__builtin_inff();
+  }
+}
+
+// Raises the maxima where a score passes one by more than kRescale, and turns scores into
+// packed probabilities (two 16-token pages a group).
+template <class T, int NT>
+__device__ __forceinline__ void weights(u4 (&p)[2 * NT], Rows &r, const f16v (&s)[NT], float sl2) {
+  // The maximum is taken of exponents (the compiler knows a product's result to be canonical;
+  // of the MFMA's it would quiet every operand first), which are formed again after it: kept
+  // across the rare branch, they and the outputs were copied on the common path (70 moves).
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, __builtin_fmaf(s[t][i], sl2, -r.m));
+  if (__builtin_expect(__any(top > r.raise), 0)) {
+    const bool fresh = r.raise < 0.f;  // no score yet: the first ones set the maximum
+    float up = fmaxf(top, other_half(top));
+    if (!fresh) up = fmaxf(up, 0.f);
+    const bool none = up == -__builtin_inff();
+    up = none ? 0.f : up;
+    const float f = fresh ? 0.f : __builtin_amdgcn_exp2f(-up);
+    r.raise = none ? r.raise : kRescale;
+    r.m += up;
+    r.l *= f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r.o[c][i] *= f;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t w = T::pack(__builtin_amdgcn_exp2f(__builtin_fmaf(s[t][2 * j], sl2, -r.m)),
+                                 __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][2 * j + 1], sl2, -r.m)));
+      p[2 * t + (j >> 2)][j & 3] = w;
+      r.l = T::add2(w, r.l);
+    }
+  // formed here, not past a barrier that follows
+#pragma unroll
+  for (int j = 0; j < 2 * NT; ++j) asm volatile("" : "+v"(p[j]));
+  asm volatile("" : "+v"(r.l));
+}
+
+template <class T, int NT, bool kTr>
+__device__ __forceinline__ void outputs(Rows &r, const Lane &ln, const u4 (&p)[2 * NT], uint32_t vbase) {
+#pragma unroll
+  for (int kk = 0; kk < 2 * NT; ++kk)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) r.o[ct] = T::mfma(value_operand<kTr>(ln, vbase, kk, ct), p[kk], r.o[ct]);
+}
+
+// The value product of a tile that is not whole for every row: a masked token has weight 0,
+// and 0 times an infinity or NaN in its value would be NaN.  A tile with such values (found
+// by a sum of all values times 0, a quarter of the product's time) enters the product
+// without them and gives true; add_odd then gives them to the rows that see their tokens.
+template <class T, int NT, bool kTr>
+__device__ __forceinline__ bool outputs_masked(Rows &r, const Lane &ln, const u4 (&p)[2 * NT], uint32_t vbase) {
+  float odd = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < 2 * NT; ++kk)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+      const u4 v = value_operand<kTr>(ln, vbase, kk, ct);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) odd = T::times0(v[j], odd);
+    }
+  const bool any = __any(odd != odd);
+#pragma unroll
+  for (int kk = 0; kk < 2 * NT; ++kk)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+      u4 v = value_operand<kTr>(ln, vbase, kk, ct);
+      if (__builtin_expect(any, 0)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] &= ~bad_halves<T>(v[j]);
+      }
+      r.o[ct] = T::mfma(v, p[kk], r.o[ct]);
+    }
+  return any;
+}
+
+// Adds the infinities and NaN among a token's four values (channels 4 i .. + 3 of group ct,
+// as the accumulators hold them) to the row's outputs.
+template <class T>
+__device__ __forceinline__ void add_odd(f16v &o, int i, u2 v) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t x = v[j >> 1] >> (16 * (j & 1)) & 0xFFFFu;
+    o[4 * i + j] += bad_halves<T>(x) & 1u ? T::widen(x) : 0.f;
+  }
+}
+
+// The value product of one 64-token tile and the key product of the next, one MFMA after the
+// other with the operands read kAhead products before (the order is pinned: left alone, the
+// compiler reads one ahead and every product waits for LDS).
+template <class T, bool kTr>
+__device__ __forceinline__ void multiply(Rows &r, f16v (&s)[2], const Lane &ln, const u4 (&p)[4], const u4 (&q)[8],
+                                         uint32_t vbase, uint32_t kbase) {
+  constexpr int kAhead = 6;
+  u4 x[kAhead];
+  auto operand = [&](int i) {
+    if (i < 16) return value_operand<kTr>(ln, vbase, i >> 2, i & 3);
+    return lds_u4(kbase + (ln.k0 ^ (((i - 16) >> 1) << 5)) + (i & 1) * 8192);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) x[i] = operand(i);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    const u4 a = x[i % kAhead];
+    if (i < 16) r.o[i & 3] = T::mfma(a, p[i >> 2], r.o[i & 3]);
+    else s[i & 1] = T::mfma(a, q[(i - 16) >> 1], s[i & 1]);
+    if (i + kAhead < 32) x[i % kAhead] = operand(i + kAhead);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+}  // namespace ta
+}  // namespace gkv
