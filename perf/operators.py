@@ -240,8 +240,10 @@ def _own_cache(case, seed, k, v):
     lens, news = _lengths(case), _news(case)
     opened = [-(-(t + n) // P) - -(-t // P) for t, n in zip(lens, news)]
     extra = max(-(-(t + n) // P) for t, n in zip(lens, news)) - -(-case["tokens"] // P)
+    # (a cache whose capacity holds no whole page has no boxes)
+    page = case["page"] if case["page"] and (case["tokens"] + extra * P) // case["page"] else 0
     cache = gkv.GradedCache.build(k.view(torch.int16), v.view(torch.int16), Hq=case["heads"],
-                                  levels=_level_table(case), page=case["page"], nres_cap=_kept(case),
+                                  levels=_level_table(case), page=page, nres_cap=_kept(case),
                                   extra_blocks=extra, slack={EXACT: sum(opened) * case["kv_heads"]},
                                   v_per_token=case["per_token"], seq_lens=lens if case["ragged"] else None)
     if _kept(case):
@@ -263,7 +265,8 @@ def run(s):
         if kind == "append":
             out = {"records": cache.arena, "certificate": cache.cert}
             if s["case"]["page"]:
-                out["boxes"] = cache.boxes
+                none = torch.empty((cache.B, cache.Hkv, 0), dtype=torch.int16, device="cuda")
+                out["boxes"] = cache.boxes if cache.page else none
             return out
         return {"out": cache.chunk_attn(s["q"], s["news"])}
     if kind == "prompt":
