@@ -202,6 +202,9 @@ typedef struct gkv_pool gkv_pool;
 gkv_pool *gkv_pool_create(const int64_t cap_host[6]);
 int64_t gkv_pool_bytes(const gkv_pool *p);
 int64_t gkv_pool_alloc(gkv_pool *p, int32_t level); /* -1 when the pool is full */
+/* n slots of one level into offsets_host[n], in the order n calls would give them, or
+ * GKV_E_POOL and none. */
+gkv_status gkv_pool_alloc_many(gkv_pool *p, int32_t level, int64_t n, int64_t *offsets_host);
 gkv_status gkv_pool_free(gkv_pool *p, int32_t level, int64_t offset);
 int64_t gkv_pool_used(const gkv_pool *p, int32_t level);
 void gkv_pool_destroy(gkv_pool *p);
@@ -414,6 +417,53 @@ typedef enum gkv_dtype { GKV_F16 = 0, GKV_BF16 = 1 } gkv_dtype;
 gkv_status gkv_prompt_attn(const void *q, const void *k, const void *v, void *out, int32_t dtype, int32_t Hkv,
                            int32_t Hq, int32_t nseq, const int64_t *len_host, int64_t q_stride, int64_t k_stride,
                            int64_t v_stride, int64_t out_stride, void *stream);
+
+/* Append n_new_host[b] >= 0 tokens to every sequence b (a chunk of its prompt, the drafts of
+ * a speculative step; 0 for a retired one): gkv_append for many tokens at once, with the
+ * same records, boxes and certificate numbers that as many calls of it leave (no
+ * demotions).  k_new, v_new: packed rows of [Hkv][128] fp16, sequence after sequence,
+ * k_stride / v_stride elements from token to token (rules as for gkv_prompt_attn).
+ * Without per-sequence lengths every n_new_host[b] is the same (GKV_E_SHAPE).  A sequence's
+ * last, partial block must be exact; the blocks a sequence opens take the slots
+ * new_koff_host / new_voff_host [n_open], listed in the order of sequence, KV head, block,
+ * and n_open is their number, Hkv * sum_b (ceil((T_b + n_b) / 64) - ceil(T_b / 64))
+ * (GKV_E_ARG).  Slots must not overlap and lie in the arena on multiples of 16 bytes.
+ * Slots at even distances are passed to the GPU as runs; a call makes one launch for
+ * every 48 runs.  GKV_E_UNSUPPORTED for more than GKV_MAX_CHUNK_SEQS sequences. */
+#define GKV_MAX_CHUNK_SEQS 128
+gkv_status gkv_append_chunk(gkv_cache *c, const uint16_t *k_new, const uint16_t *v_new, int64_t k_stride,
+                            int64_t v_stride, const int32_t *n_new_host, const int64_t *new_koff_host,
+                            const int64_t *new_voff_host, int32_t n_open, void *stream);
+
+/* Drop the newest tokens (drafts that were rejected): sequence b keeps its first
+ * len_host[b] (0 <= len_host[b] <= its length; ignored for a retired sequence; the same
+ * for all without per-sequence lengths).  The dropped blocks' slots (host offset mirrors
+ * koff_host / voff_host [B][Hkv][nblk_cap]) go back to pool, the next append's first;
+ * they are reusable by later work on `stream`.  The dropped rows of a block that stays
+ * become zero; its certificate number vmax stays (a bound).  A block that stays without
+ * being filled must be exact (GKV_E_SHAPE: tokens of a demoted block cannot be dropped
+ * apart).  GKV_E_UNSUPPORTED for a cache with residual rows, which may be rows of
+ * dropped tokens. */
+gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, const int64_t *voff_host,
+                        const int64_t *len_host, void *stream);
+
+/* Attention of the newest tokens over the cache: the n_new_host[b] >= 0 newest tokens of every
+ * sequence b (appended before: a prompt's chunk, a speculative step's drafts, one token),
+ * query head g of the one at position t reading every cached token 0 .. t of KV head g / G
+ * at its block's level, residual rows overriding their tokens' graded entries,
+ *   out[i][g][:] = sum_{j <= t} softmax_j(q_ig . k_j / sqrt(128)) v_j.
+ * q, out: packed rows of [Hq][128] fp16, sequence after sequence, q_stride / out_stride
+ * elements from token to token (rules as for gkv_prompt_attn); out must not overlap q.
+ * Graded entries are decoded to fp16 (one rounding of code * scale + zero) and
+ * probabilities enter the value product in fp16; logits, maxima and sums are fp32.  A token
+ * that a row does not see has no effect on it, whatever it holds.  n_new_host[b] is at most
+ * the sequence's length (GKV_E_SHAPE) and 0 for a retired one (GKV_E_ARG).
+ * ws: gkv_chunk_ws_bytes(c, n_new_host) bytes (16-byte aligned, no initialisation; may be
+ * NULL when that is 0), which depends on the lengths (-1: the call would be refused).
+ * GKV_E_UNSUPPORTED for more than GKV_MAX_CHUNK_SEQS sequences. */
+int64_t gkv_chunk_ws_bytes(const gkv_cache *c, const int32_t *n_new_host);
+gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const gkv_cache *c, const int32_t *n_new_host,
+                          uint16_t *out, int64_t out_stride, void *ws, int64_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------- multi-layer service */
 

@@ -95,6 +95,11 @@ _observe = _sig("gkv_observe_mass", _i32,
 _query_norms = _sig("gkv_query_norms", _i32, [_vp, _i32, _i32, _i32, _i32, _vp, _vp])
 _allocate = _sig("gkv_allocate_levels", _i32,
                  [_vp, _vp, _vp, _i32, _i32, _i64, ctypes.c_double, ctypes.c_double, _i32, _i32, _vp, _vp])
+_pool_alloc_many = _sig("gkv_pool_alloc_many", _i32, [_vp, _i32, _i64, _vp])
+_append_chunk = _sig("gkv_append_chunk", _i32, [_P(CacheStruct), _vp, _vp, _i64, _i64, _vp, _vp, _vp, _i32, _vp])
+_truncate = _sig("gkv_truncate", _i32, [_P(CacheStruct), _vp, _vp, _vp, _vp, _vp])
+_chunk_ws = _sig("gkv_chunk_ws_bytes", _i64, [_P(CacheStruct), _vp])
+_chunk_attn = _sig("gkv_chunk_attn", _i32, [_vp, _i64, _P(CacheStruct), _vp, _vp, _i64, _vp, _i64, _vp])
 _prompt_attn = _sig("gkv_prompt_attn", _i32, [_vp] * 4 + [_i32] * 4 + [_vp] + [_i64] * 4 + [_vp])
 ROUNDING = {"up": 0, "nearest": 1}
 
@@ -107,6 +112,8 @@ EXPORTED = [
     "gkv_observe_ws_bytes", "gkv_observe_mass", "gkv_query_norms", "gkv_allocate_levels", "gkv_layers_step",
     "gkv_cache_changed", "gkv_graded_decode_attn_noalloc", "gkv_noalloc_scratch_bytes", "gkv_retire_sequence",
     "gkv_admit_sequence", "gkv_stream_read_probe", "gkv_prompt_attn",
+    "gkv_pool_alloc_many", "gkv_append_chunk", "gkv_truncate",
+    "gkv_chunk_ws_bytes", "gkv_chunk_attn",
 ]
 
 
@@ -311,6 +318,12 @@ class Pool:
         if off < 0:
             raise GkvError(-1, f"pool exhausted for level {level}")
         return off
+
+    def alloc_many(self, level, n):
+        """n slots of one level, or GkvError and none."""
+        out = np.empty(n, dtype=np.int64)
+        _check(_pool_alloc_many(self.h, level, n, _np_ptr(out)), "pool_alloc_many")
+        return out
 
     def free(self, level, off):
         _check(_pool_free(self.h, level, int(off)), "pool_free")
@@ -597,24 +610,102 @@ class GradedCache:
             blk = int(lens[b]) // P
             self.koff_host[b, :, blk] = nk[b * self.Hkv:(b + 1) * self.Hkv]
             self.voff_host[b, :, blk] = nv[b * self.Hkv:(b + 1) * self.Hkv]
-        moves = []
-        if profile is not None:
-            jobs = np.empty(3 * 64, dtype=np.int32)
-            to = np.empty(64, dtype=np.int8)
+        return self._cross(profile) if profile is not None else []
+
+    def _cross(self, profile):
+        """Demotes every block whose level the ladder profile lowers at the present lengths;
+        returns [(b, h, blk, old, new)]."""
+        jobs = np.empty(3 * 64, dtype=np.int32)
+        to = np.empty(64, dtype=np.int8)
+        n = _ladder_crossings(ctypes.byref(self.c), PROFILES.get(profile, profile), self.T, _np_ptr(jobs),
+                              _np_ptr(to), 64)
+        if n < 0:
+            raise GkvError(n, "ladder_crossings")
+        if n > 64:
+            jobs = np.empty(3 * n, dtype=np.int32)
+            to = np.empty(n, dtype=np.int8)
             n = _ladder_crossings(ctypes.byref(self.c), PROFILES.get(profile, profile), self.T, _np_ptr(jobs),
-                                  _np_ptr(to), 64)
-            if n < 0:
-                raise GkvError(n, "ladder_crossings")
-            if n > 64:
-                jobs = np.empty(3 * n, dtype=np.int32)
-                to = np.empty(n, dtype=np.int8)
-                n = _ladder_crossings(ctypes.byref(self.c), PROFILES.get(profile, profile), self.T, _np_ptr(jobs),
-                                      _np_ptr(to), n)
-            J = jobs[: 3 * n].reshape(n, 3)
-            olds = [int(self.level_host[b, h, i]) for b, h, i in J]
-            self.demote([tuple(x) for x in J], to[:n])
-            moves = [(int(b), int(h), int(i), o, int(t)) for (b, h, i), o, t in zip(J, olds, to[:n])]
-        return moves
+                                  _np_ptr(to), n)
+        J = jobs[: 3 * n].reshape(n, 3)
+        olds = [int(self.level_host[b, h, i]) for b, h, i in J]
+        self.demote([tuple(x) for x in J], to[:n])
+        return [(int(b), int(h), int(i), o, int(t)) for (b, h, i), o, t in zip(J, olds, to[:n])]
+
+    def _counts(self, lens, what, dtype):
+        """One number per sequence as a contiguous array (an int: the same for all)."""
+        a = np.asarray(lens)
+        if a.ndim == 0:
+            a = np.full(self.B, a)
+        if a.shape != (self.B,) or a.dtype.kind not in "iu":
+            raise GkvError(-2, what)
+        if a.size and (int(a.max()) > np.iinfo(dtype).max or int(a.min()) < np.iinfo(dtype).min):
+            raise GkvError(-2, what)
+        return np.ascontiguousarray(a, dtype=dtype)
+
+    def append_chunk(self, k_new, v_new, lens, profile=None):
+        """gkv_append_chunk: append lens[b] tokens to every sequence (k_new, v_new packed fp16
+        rows [n][Hkv][128], n = sum of lens; views with a token stride are read in place);
+        then, with a ladder profile, demote what it lowers.  Returns the demotions
+        [(b, h, blk, old, new)]."""
+        kd, vd = _rows_dev(k_new, "append_chunk", self._dev), _rows_dev(v_new, "append_chunk", self._dev)
+        lens = self._counts(lens, "append_chunk", np.int32)
+        if kd.dtype != torch.float16 or vd.dtype != torch.float16:
+            raise GkvError(-1, "append_chunk")
+        if kd.shape != vd.shape or kd.shape[1] != self.Hkv or kd.shape[0] != int(lens.sum(dtype=np.int64)):
+            raise GkvError(-2, "append_chunk")
+        have = self.lengths()
+        first = -(-np.maximum(have, 0) // P)
+        last = np.where(lens > 0, -(-(have + lens) // P), first)
+        opened = (last - first).tolist()
+        n = sum(opened) * self.Hkv
+        # K and V slots of one block side by side, sequence by sequence
+        kv = self.pool.alloc_many(EXACT, 2 * n) if n > 0 else np.empty(0, np.int64)
+        nk, nv = kv[0::2].copy(), kv[1::2].copy()
+        st = _append_chunk(ctypes.byref(self.c), _dptr(kd), _dptr(vd), _row_stride(kd), _row_stride(vd),
+                           _np_ptr(lens), _np_ptr(nk), _np_ptr(nv), n, _stream())
+        if st != 0:
+            for off in kv[::-1]:
+                self.pool.free(EXACT, int(off))
+            raise GkvError(st, "append_chunk")
+        i = 0
+        for b, m in enumerate(opened):  # the mirrors follow the library only once the call succeeded
+            if m > 0:
+                at = (b, slice(None), slice(int(first[b]), int(last[b])))
+                self.koff_host[at] = nk[i:i + m * self.Hkv].reshape(self.Hkv, m)
+                self.voff_host[at] = nv[i:i + m * self.Hkv].reshape(self.Hkv, m)
+                i += m * self.Hkv
+        return self._cross(profile) if profile is not None else []
+
+    def truncate(self, lens):
+        """gkv_truncate: every sequence keeps its first lens[b] tokens (-1 for a retired one)."""
+        lens = self._counts(lens, "truncate", np.int64)
+        _check(_truncate(ctypes.byref(self.c), self.pool.h, _np_ptr(self.koff_host), _np_ptr(self.voff_host),
+                         _np_ptr(lens), _stream()), "truncate")
+
+    def chunk_attn(self, q, lens, out=None, ws=None):
+        """gkv_chunk_attn: attention of the lens[b] newest tokens of every sequence over the
+        cache they were appended to (q packed fp16 rows [n][Hq][128], n = sum of lens).
+        Returns out [n][Hq][128] fp16."""
+        q = _rows_dev(q, "chunk_attn", self._dev)
+        lens = self._counts(lens, "chunk_attn", np.int32)
+        if q.dtype != torch.float16:
+            raise GkvError(-1, "chunk_attn")
+        n = int(lens.sum(dtype=np.int64))
+        if q.shape[0] != n or q.shape[1] != self.Hq:
+            raise GkvError(-2, "chunk_attn")
+        if out is None:
+            out = torch.empty((n, self.Hq, D), dtype=torch.float16, device=self._dev)
+        elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or (
+                n and (out.stride(2) != 1 or out.stride(1) != D)):
+            raise GkvError(-2, "chunk_attn")
+        if ws is None:
+            # of this call alone: its size goes by the lengths, and a captured graph keeps its own
+            nb = int(_chunk_ws(ctypes.byref(self.c), _np_ptr(lens)))
+            ws = torch.empty(nb, dtype=torch.uint8, device=self._dev) if nb > 0 else None
+        _check(_chunk_attn(_dptr(q), _row_stride(q), ctypes.byref(self.c), _np_ptr(lens), _dptr(out),
+                           _row_stride(out), _dptr(ws), ws.numel() if ws is not None else 0, _stream()),
+               "chunk_attn")
+        return out
 
     def quest_select(self, q, topk, out=None):
         q = _as_bits(q, self._dev)

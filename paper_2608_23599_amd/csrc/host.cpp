@@ -175,6 +175,14 @@ extern "C" int64_t gkv_pool_alloc(gkv_pool *p, int32_t level) {
   return p->base[i] + s * block_bytes(level);
 }
 
+extern "C" gkv_status gkv_pool_alloc_many(gkv_pool *p, int32_t level, int64_t n, int64_t *offsets) {
+  const int i = level_slot(level);
+  if (!p || i < 0 || n < 0 || (n && !offsets)) return GKV_E_ARG;
+  if ((int64_t)p->free_list[i].size() < n) return GKV_E_POOL;
+  for (int64_t k = 0; k < n; ++k) offsets[k] = gkv_pool_alloc(p, level);
+  return GKV_OK;
+}
+
 extern "C" gkv_status gkv_pool_free(gkv_pool *p, int32_t level, int64_t off) {
   const int i = level_slot(level);
   if (!p || i < 0) return GKV_E_ARG;

@@ -149,25 +149,20 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParam
     ta::multiply<T, true>(st, s, ln, pr, q, values(t), keys(t + 1));
     after(t);
   }
-  bool odd = false;  // some value there is infinite or NaN
+  ta::u4 odd = {0, 0, 0, 0};  // infinities and NaN there
   for (;; ++t) {
-    ta::mask_scores<2>(s, ln, seen(t));
+    const uint64_t vis = seen(t);
+    ta::mask_scores<2>(s, ln, vis);
     ta::weights<T, 2>(pr, st, s, p.sl2);
     before(t);
-    odd |= ta::outputs_masked<T, 2, true>(st, ln, pr, values(t));
+    const bool clean = ta::find_odd<T, 2, true>(ln, values(t), vis, odd);
+    ta::outputs_clean<T, 2, true>(st, ln, pr, values(t), clean);
     if (t == ntile - 1) break;
     ta::scores<T, 2>(s, ln, q, keys(t + 1));
     after(t);
   }
   if (!second) meet();
-  if (__builtin_expect(odd, 0))
-    for (int x = full * kTile; x <= tok; ++x) {
-      const uint16_t *vp = p.v + (start + x) * p.vs + (int64_t)h * D + 4 * ln.hf;
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ta::add_odd<T>(st.o[c], i, *(const ta::u2 *)(vp + 32 * c + 8 * i));
-    }
+  ta::add_odd(st, odd);
   if (row < rows) {
     const float l = st.l + ta::other_half(st.l);
     const float inv = l > 0.f ? 1.f / l : l;  // (a NaN stays)

@@ -46,7 +46,7 @@ constexpr int kRows = 32;          // rows of a wavefront
 constexpr float kRescale = 8.0f;   // lazy rescale threshold (log2 units)
 
 struct F16 {
-  static constexpr uint32_t kExp = 0x7C007C00u;  // exponent bits of a pair
+  static constexpr uint32_t kInf = 0x7C00u, kExp = 0x7C007C00u;  // infinity; the exponent bits of a pair
   __device__ static f16v mfma(u4 a, u4 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0,
                                                   0);
@@ -69,10 +69,9 @@ struct F16 {
     none[0] = none[1] = (_Float16)0.0f;
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, p), none, acc, false);
   }
-  __device__ static float widen(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
 };
 struct BF16 {
-  static constexpr uint32_t kExp = 0x7F807F80u;
+  static constexpr uint32_t kInf = 0x7F80u, kExp = 0x7F807F80u;
   __device__ static f16v mfma(u4 a, u4 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
   }
@@ -92,7 +91,6 @@ struct BF16 {
     none[0] = none[1] = (__bf16)0.0f;
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, p), none, acc, false);
   }
-  __device__ static float widen(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
 };
 
 // ---------------------------------------------------------------- LDS tiles
@@ -210,13 +208,13 @@ __device__ __forceinline__ void weights(u4 (&p)[2 * NT], Rows &r, const f16v (&s
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, __builtin_fmaf(s[t][i], sl2, -r.m));
   if (__builtin_expect(__any(top > r.raise), 0)) {
-    const bool fresh = r.raise < 0.f;  // no score yet: the first ones set the maximum
-    float up = fmaxf(top, other_half(top));
-    if (!fresh) up = fmaxf(up, 0.f);
-    const bool none = up == -__builtin_inff();
-    up = none ? 0.f : up;
-    const float f = fresh ? 0.f : __builtin_amdgcn_exp2f(-up);
-    r.raise = none ? r.raise : kRescale;
+    // only the rows that pass their own limit (one that has seen no score: at the first ones),
+    // so that a row's rounding does not depend on its neighbours'
+    const float high = fmaxf(top, other_half(top));
+    const bool go = high > r.raise;
+    const float up = go ? high : 0.f;
+    const float f = r.raise < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
+    r.raise = go ? kRescale : r.raise;
     r.m += up;
     r.l *= f;
 #pragma unroll
@@ -247,44 +245,82 @@ __device__ __forceinline__ void outputs(Rows &r, const Lane &ln, const u4 (&p)[2
     for (int ct = 0; ct < 4; ++ct) r.o[ct] = T::mfma(value_operand<kTr>(ln, vbase, kk, ct), p[kk], r.o[ct]);
 }
 
-// The value product of a tile that is not whole for every row: a masked token has weight 0,
-// and 0 times an infinity or NaN in its value would be NaN.  A tile with such values (found
-// by a sum of all values times 0, a quarter of the product's time) enters the product
-// without them and gives true; add_odd then gives them to the rows that see their tokens.
+// Values (token t, channels 32 ct + 8 j + 4 hf .. + 3) of a tile.
+template <bool kTr>
+__device__ __forceinline__ u2 value_quad(int hf, uint32_t vbase, int t, int ct, int j) {
+  if constexpr (kTr) {
+    return *(__attribute__((address_space(3))) const u2 *)(uintptr_t)(vbase + value_place(t, 4 * ct + j) + 8 * hf);
+  } else {
+    const uint32_t at = vbase + ((t >> 4) * 4 + ct) * 1024 + 512 * ((t >> 2) & 1) + 8 * ((t >> 3) & 1) + 2 * (t & 3) +
+                        16 * (8 * j + 4 * hf);
+    uint32_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)(at + 16 * i);
+    return u2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+  }
+}
+
+// A tile that is not whole for every row: a masked token has weight 0, and 0 times an
+// infinity or NaN in its value would be NaN.  Finds whether a tile holds such values (a sum of
+// all values times 0, a quarter of the product's time); if so they must not enter the
+// product, and `odd` keeps, two bits for each of the lane's 64 outputs, which of them the
+// row sees (1 infinity, 2 -infinity, 3 both or NaN), for add_odd to add in the end.
 template <class T, int NT, bool kTr>
-__device__ __forceinline__ bool outputs_masked(Rows &r, const Lane &ln, const u4 (&p)[2 * NT], uint32_t vbase) {
-  float odd = 0.f;
+__device__ __forceinline__ bool find_odd(const Lane &ln, uint32_t vbase, uint64_t vis, u4 &odd) {
+  float zero = 0.f;
 #pragma unroll
   for (int kk = 0; kk < 2 * NT; ++kk)
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) {
       const u4 v = value_operand<kTr>(ln, vbase, kk, ct);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) odd = T::times0(v[j], odd);
+      for (int j = 0; j < 4; ++j) zero = T::times0(v[j], zero);
     }
-  const bool any = __any(odd != odd);
+  const bool any = __any(zero != zero);
+  if (__builtin_expect(any, 0)) {
+    int hf = ln.hf;  // (opaque: no address of this path is kept in a register through the loop)
+    asm volatile("" : "+s"(vbase), "+v"(hf));
+#pragma unroll 1
+    for (int t = 0; t < 32 * NT; ++t) {
+      const uint32_t seen = (vis >> t) & 1 ? 3u : 0u;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const u2 v = value_quad<kTr>(hf, vbase, t, i >> 2, i & 3);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t x = v[k >> 1] >> (16 * (k & 1)) & 0xFFFFu, e = x & 0x7FFFu;
+          const uint32_t b = e < T::kInf ? 0u : e > T::kInf ? 3u : x == e ? 1u : 2u;
+          odd[i >> 2] |= (b & seen) << (8 * (i & 3) + 2 * k);
+        }
+      }
+    }
+  }
+  return any;
+}
+
+// The value product without infinities and NaN where `clean` (wave-uniform).
+template <class T, int NT, bool kTr>
+__device__ __forceinline__ void outputs_clean(Rows &r, const Lane &ln, const u4 (&p)[2 * NT], uint32_t vbase,
+                                              bool clean) {
 #pragma unroll
   for (int kk = 0; kk < 2 * NT; ++kk)
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) {
       u4 v = value_operand<kTr>(ln, vbase, kk, ct);
-      if (__builtin_expect(any, 0)) {
+      if (__builtin_expect(clean, 0)) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] &= ~bad_halves<T>(v[j]);
       }
       r.o[ct] = T::mfma(v, p[kk], r.o[ct]);
     }
-  return any;
 }
 
-// Adds the infinities and NaN among a token's four values (channels 4 i .. + 3 of group ct,
-// as the accumulators hold them) to the row's outputs.
-template <class T>
-__device__ __forceinline__ void add_odd(f16v &o, int i, u2 v) {
+__device__ __forceinline__ void add_odd(Rows &r, const u4 &odd) {
+  if (__builtin_expect(!__any(odd[0] | odd[1] | odd[2] | odd[3]), 1)) return;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t x = v[j >> 1] >> (16 * (j & 1)) & 0xFFFFu;
-    o[4 * i + j] += bad_halves<T>(x) & 1u ? T::widen(x) : 0.f;
+  for (int i = 0; i < 64; ++i) {
+    const uint32_t b = odd[i >> 4] >> (2 * (i & 15)) & 3u;
+    r.o[i >> 4][i & 15] += b == 0 ? 0.f : b == 3 ? __builtin_nanf("") : b == 1 ? __builtin_inff() : -__builtin_inff();
   }
 }
 
