@@ -2,17 +2,16 @@
 // drafts) over the graded cache (sections 3.1, 3.2, 3.4 and 3.7): the many-query form of the
 // dense decode read.
 //
-// The records are decoded to fp16 tiles in LDS (one rounding of code * scale + zero), the form
-// that the row tiles of tile_attn.h read.  Two shapes of workgroup:
-//  * shared (kWaves row groups): the wavefronts hold 32 rows each and share every tile, so
-//    a record is decoded once for all of a workgroup's rows;
-//  * private (at most 32 rows of a (sequence, KV head)): every wavefront holds all the rows
-//    and takes half blocks of its own, without barriers, and the wavefronts' states are
-//    merged at the end.
-// Either splits a long context over workgroups whose partials a merge kernel joins.
+// Two ways, chosen for each sequence by its rows (tokens times heads of a group):
+//  * few rows: every wavefront holds all of a (sequence, KV head)'s rows, reads whole blocks of its
+//    own straight from the records into operands, and decodes them there;
+//  * many rows: the cache is decoded once to fp16 tiles in the workspace, over which row tiles
+//    go as a prompt's do (tile_attn.h).
+// Either splits a long context over workgroups whose partials a merge kernel joins.  A graded
+// value is rounded to fp16 once, code * scale + zero in one step.
 #include <hip/hip_runtime.h>
 
-#include <new>
+#include <algorithm>
 
 #include "gkv_internal.h"
 #include "tile_attn.h"
@@ -40,23 +39,33 @@ struct ChunkParams {
   const int64_t *koff, *voff;
   const uint8_t *arena;
   const uint64_t *res_mask;  // null without residual rows
-  const int32_t *res_idx;
+  const int32_t *res_idx, *res_off;
   const uint8_t *res_rows;
   int32_t nblk_cap, Hkv, G, nseq, nres, nres_cap, nrb_cap, vtok;
   float sl2;
   int64_t part0;             // first partial row of this launch
-  int32_t seq[kMaxSeqs];     // sequence
+  uint8_t *list;             // many rows: the decoded tiles
+  int32_t *whole;            // and how many of each list every row sees whole
+  int32_t list0[kMaxSeqs];   // first tile of a sequence's lists (one a KV head)
   int32_t T[kMaxSeqs], n[kMaxSeqs];  // its tokens, and the newest ones that attend
   int32_t row0[kMaxSeqs];    // their first packed row
-  int32_t split[kMaxSeqs];   // workgroups that share a row tile's context
+  uint16_t split[kMaxSeqs];  // workgroups that share a row tile's context
+  uint8_t seq[kMaxSeqs];     // sequence
   int32_t wg0[kMaxSeqs + 1]; // workgroups per KV head before each
 };
 
 // ---------------------------------------------------------------- records to tiles
-__device__ __forceinline__ int64_t uni64(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
-  return (int64_t)(((uint64_t)hi << 32) | lo);
+// Table entries are the same for a whole wavefront and no kernel here writes them: scalar loads,
+// which wait apart from the records' vector loads (as vector loads they stood in line with
+// those, and every block waited for its table entries alone: 241 us against XXX for 2 tokens
+// over 8 x 128k).
+typedef const __attribute__((address_space(4))) uint64_t *ScalarU64;
+typedef const __attribute__((address_space(4))) uint32_t *ScalarU32;
+__device__ __forceinline__ uint64_t table64(const void *t, int64_t i) { return ((ScalarU64)(uintptr_t)t)[i]; }
+__device__ __forceinline__ uint32_t table32(const void *t, int64_t i) { return ((ScalarU32)(uintptr_t)t)[i]; }
+__device__ __forceinline__ int table8(const int8_t *t, int64_t i) {  // by the word it lies in
+  const uintptr_t at = (uintptr_t)t + i;
+  return *(ScalarU32)(at & ~(uintptr_t)3) >> (8 * (at & 3)) & 0xFFu;
 }
 
 // A block, or 64 residual rows, as it is read (wave-uniform).
@@ -70,10 +79,10 @@ __device__ __forceinline__ Visit visit_at(const ChunkParams &p, int64_t u, int v
   Visit x;
   if (v < nblk) {
     const int64_t ti = u * p.nblk_cap + v;
-    x.level = __builtin_amdgcn_readfirstlane((int)p.level[ti]);
-    x.k = p.arena + uni64(p.koff[ti]);
-    x.v = p.arena + uni64(p.voff[ti]);
-    x.drop = p.res_mask ? (uint64_t)uni64((int64_t)p.res_mask[ti]) : 0;
+    x.level = table8(p.level, ti);
+    x.k = p.arena + table64(p.koff, ti);
+    x.v = p.arena + table64(p.voff, ti);
+    x.drop = p.res_mask ? table64(p.res_mask, ti) : 0;
   } else {
     const int r = v - nblk;
     x.level = GKV_EXACT;
@@ -110,7 +119,7 @@ __device__ __forceinline__ void load_raw(Raw &x, const uint8_t *rec, int level, 
     x.w[0][1] = s[1];
   } else if (TENSOR == GKV_KEYS) {
     const uint16_t *c = (const uint16_t *)rec + 8 * kg;
-    if (level == GKV_CENTROID) c += (*(const uint32_t *)(rec + KC * D * 2 + 4 * pg) >> (2 * m) & 3u) * D;
+    if (level == GKV_CENTROID) c += (table32(rec + KC * D * 2, pg) >> (2 * m) & 3u) * D;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x.w[i] = *(const u4 *)(c + 32 * i);
   } else if (level == GKV_CENTROID) {
@@ -213,33 +222,36 @@ __device__ __forceinline__ void stage_value_codes(uint32_t (&y)[16], const Raw &
   }
 }
 
-// A lane's chunk of page pg into the key tile (row pg_at * 16 + m of the tile).
-__device__ __forceinline__ void stage_keys(const Raw &x, int level, uint32_t head, uint32_t tile, int pg_at, int lane) {
-  const int kg = lane >> 4, m = lane & 15;
-  uint32_t y[16];
-  if (level == GKV_INT8) stage_key_codes<8>(y, x, head, kg);
-  else if (level == GKV_INT4) stage_key_codes<4>(y, x, head, kg);
-  else if (level == GKV_INT2) stage_key_codes<2>(y, x, head, kg);
-  else
+// A lane's key chunk of a page as fp16 pairs: words 4 j .. 4 j + 3 are channels 32 j + 8 kg .. + 7.
+template <int LEVEL>
+__device__ __forceinline__ void key_words(uint32_t (&y)[16], const Raw &x, uint32_t head, int kg) {
+  if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
+    stage_key_codes<LEVEL>(y, x, head, kg);
+  } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = x.w[i >> 2][i & 3];
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    *(LdsW4)(uintptr_t)(tile + ta::key_place(16 * pg_at + m, 4 * j + kg)) =
-        u4{y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]};
+  }
 }
 
-// The same for the value tile (operand form); drop: the block's tokens that are not read,
-// whose values become zero (their weight is zero, but 0 * infinity is NaN).
-__device__ __forceinline__ void stage_values(const Raw &x, int level, const uint8_t *rec, uint64_t drop, uint32_t head,
-                                             uint32_t tile, int pg, int pg_at, int lane, bool vtok) {
-  const int kg = lane >> 4, m = lane & 15;
-  uint32_t y[16];
-  if (level == GKV_INT8) stage_value_codes<8>(y, x, head, pg, lane, vtok);
-  else if (level == GKV_INT4) stage_value_codes<4>(y, x, head, pg, lane, vtok);
-  else if (level == GKV_INT2) stage_value_codes<2>(y, x, head, pg, lane, vtok);
-  else if (level == GKV_CENTROID) {
-    const uint32_t ids = *(const uint32_t *)(rec + KC * D * 2 + 4 * pg) >> (8 * kg);  // of the lane's four tokens
+// The same of any level.
+__device__ __forceinline__ void key_words_any(uint32_t (&y)[16], const Raw &x, int level, uint32_t head, int kg) {
+  if (level == GKV_INT8) key_words<GKV_INT8>(y, x, head, kg);
+  else if (level == GKV_INT4) key_words<GKV_INT4>(y, x, head, kg);
+  else if (level == GKV_INT2) key_words<GKV_INT2>(y, x, head, kg);
+  else key_words<GKV_EXACT>(y, x, head, kg);
+}
+
+// A lane's value chunk of page pg as fp16 pairs: words 2 c and 2 c + 1 are tokens 4 kg .. + 3 of
+// channel 16 c + m.  drop: the block's tokens that are not read, whose values become zero
+// (their weight is zero, but 0 * infinity is NaN).
+template <int LEVEL>
+__device__ __forceinline__ void value_words(uint32_t (&y)[16], const Raw &x, const uint8_t *rec, uint64_t drop,
+                                            uint32_t head, int pg, int lane, bool vtok) {
+  const int kg = lane >> 4;
+  if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
+    stage_value_codes<LEVEL>(y, x, head, pg, lane, vtok);
+  } else if constexpr (LEVEL == GKV_CENTROID) {
+    const uint32_t ids = table32(rec + KC * D * 2, pg) >> (8 * kg);  // of the lane's four tokens
     uint32_t sel[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -251,7 +263,7 @@ __device__ __forceinline__ void stage_values(const Raw &x, int level, const uint
       const int c = q >> 1;
       y[q] = __builtin_amdgcn_perm(x.w[c >> 1][2 * (c & 1) + 1], x.w[c >> 1][2 * (c & 1)], sel[q & 1]);
     }
-  } else if (level == GKV_MEAN) {
+  } else if constexpr (LEVEL == GKV_MEAN) {
 #pragma unroll
     for (int q = 0; q < 16; ++q) y[q] = x.w[q >> 3][(q >> 1) & 3];
   } else {
@@ -265,9 +277,19 @@ __device__ __forceinline__ void stage_values(const Raw &x, int level, const uint
 #pragma unroll
     for (int q = 0; q < 16; ++q) y[q] &= keep[q & 1];
   }
-  const uint32_t at = tile + pg_at * 4096 + (kg & 1) * 512 + m * 16 + (kg >> 1) * 8;
-#pragma unroll
-  for (int c = 0; c < 8; ++c) *(LdsW2)(uintptr_t)(at + (c >> 1) * 1024 + (c & 1) * 256) = u2{y[2 * c], y[2 * c + 1]};
+}
+
+// The same of any level.
+__device__ __forceinline__ void value_words_any(uint32_t (&y)[16], const Raw &x, const Visit &v, uint32_t head, int pg,
+                                                int lane, bool vtok) {
+#define GKV_WORDS(lv) value_words<lv>(y, x, v.v, v.drop, head, pg, lane, vtok)
+  if (v.level == GKV_INT8) GKV_WORDS(GKV_INT8);
+  else if (v.level == GKV_INT4) GKV_WORDS(GKV_INT4);
+  else if (v.level == GKV_INT2) GKV_WORDS(GKV_INT2);
+  else if (v.level == GKV_CENTROID) GKV_WORDS(GKV_CENTROID);
+  else if (v.level == GKV_MEAN) GKV_WORDS(GKV_MEAN);
+  else GKV_WORDS(GKV_EXACT);
+#undef GKV_WORDS
 }
 
 // ---------------------------------------------------------------- rows
@@ -364,12 +386,184 @@ __device__ __forceinline__ uint64_t seen_by(const ChunkParams &p, const Job &j, 
 __device__ __forceinline__ bool whole_at(const ChunkParams &p, const Job &j, int v, int pos) {
   if (v < j.nblk) return v * P + P - 1 <= pos;
   const int last = min(P, p.nres - (v - j.nblk) * P) - 1;
-  return __builtin_amdgcn_readfirstlane(p.res_idx[j.u * p.nres_cap + (v - j.nblk) * P + last]) <= pos;
+  return (int)table32(p.res_idx, j.u * p.nres_cap + (v - j.nblk) * P + last) <= pos;
 }
 
-// ---------------------------------------------------------------- shared tiles
+// ---------------------------------------------------------------- many rows
+// The cache of a (sequence, KV head) as a list of tiles (ta::attend's, 64 tokens each) in the
+// workspace, decoded once for all row tiles:
+//   the blocks before block c0 = pos0 / 64, which every row sees whole, but for one-centroid
+//   ones | the residual rows of tokens before 64 c0 | the one-centroid blocks before c0, one
+//   key each | the blocks from c0 on, each with its residual tokens in their places.
+// A tile is 16 KB of keys, 16 KB of values and 64 floats that its scores start from: 0, minus
+// infinity for a place that holds no token (a residual token's in its block, those behind
+// the last row), log2(n) in a score's units for a one-centroid block, whose key counts for
+// its n tokens that are no residual ones.
+constexpr int kListTile = 2 * ta::kTileBytes + ta::kBiasBytes;
+
+// Room of a list: a tile for every block and for every 64 residual rows.
+__host__ __device__ __forceinline__ int list_tiles(int T, int nres) { return (T + P - 1) / P + (nres + P - 1) / P; }
+__device__ __forceinline__ int list_tiles(const ChunkParams &p, int T) { return list_tiles(T, p.nres); }
+
+struct ListShape {  // of one (sequence, KV head)
+  int plain, res, means;  // tiles of the first two parts, one-centroid blocks
+  int whole;              // tiles before block c0's
+};
+__device__ __forceinline__ ListShape list_shape(const ChunkParams &p, int c0, int means) {
+  ListShape l;
+  l.means = means;
+  l.plain = c0 - means;
+  l.res = (p.nres + P - 1) / P;
+  l.whole = l.plain + l.res + (means + P - 1) / P;
+  return l;
+}
+
+// One workgroup a block or 64 residual rows; a wavefront a page.  Bound by the bytes it writes.
+__global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
+  __shared__ __align__(16) uint8_t sh[1024 + 64];
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)sh;
+  const int s = blockIdx.z, h = blockIdx.y, v = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, pg = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = lane >> 4, m = lane & 15;
+  const int T = p.T[s], nblk = (T + P - 1) / P, c0 = (T - p.n[s]) / P;
+  if (v >= nblk + (p.nres + P - 1) / P) return;
+  const int64_t u = (int64_t)p.seq[s] * p.Hkv + h;
+  // one-centroid blocks before this one, and before c0
+  const int8_t *levels = p.level + u * p.nblk_cap;
+  int here = 0, all = 0;
+  for (int i = tid; i < c0; i += 256)
+    if (levels[i] == GKV_MEAN) {
+      ++all;
+      here += i < v;
+    }
+  for (int k = 32; k; k >>= 1) {
+    all += __shfl_xor(all, k);
+    here += __shfl_xor(here, k);
+  }
+  int *sums = (int *)(sh + 1024);
+  if (lane == 0) {
+    sums[2 * pg] = all;
+    sums[2 * pg + 1] = here;
+  }
+  __syncthreads();
+  all = sums[0] + sums[2] + sums[4] + sums[6];
+  here = sums[1] + sums[3] + sums[5] + sums[7];
+  const ListShape l = list_shape(p, c0, all);
+  uint8_t *list = p.list + (p.list0[s] + (int64_t)h * list_tiles(p, T)) * kListTile;
+  if (v == 0 && tid == 0) p.whole[s * p.Hkv + h] = l.whole;
+  const Visit x = visit_at(p, u, v, nblk);
+  if (v < c0 && x.level == GKV_MEAN) {  // a row of the one-centroid tiles
+    if (pg) return;
+    uint8_t *tile = list + (int64_t)(l.plain + l.res + (here >> 6)) * kListTile;
+    // the last one's workgroup also writes the places behind it
+    const int end = here == l.means - 1 ? ((here >> 6) + 1) * P : here + 1;
+    for (int r = here; r < end; ++r) {
+      const int t = r & (P - 1), n = r == here ? P - __popcll(x.drop) : 0;
+      const u4 none = {0, 0, 0, 0};
+      if (lane < 16) *(u4 *)(tile + ta::key_place(t, lane)) = n ? ((const u4 *)x.k)[lane] : none;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int d = lane + 64 * i;
+        const int at = ((t >> 4) * 4 + (d >> 5)) * 1024 + 512 * ((t >> 2) & 1) + 16 * (d & 31) + 8 * ((t >> 3) & 1) + 2 * (t & 3);
+        *(uint16_t *)(tile + ta::kTileBytes + at) = n ? ((const uint16_t *)x.v)[d] : 0;
+      }
+      if (lane == 0)
+        ((float *)(tile + 2 * ta::kTileBytes))[t] = n ? __builtin_amdgcn_logf((float)n) / p.sl2 : -__builtin_inff();
+    }
+    return;
+  }
+  const int at = v < c0 ? v - here : v < nblk ? l.whole + v - c0 : l.plain + v - nblk;
+  uint8_t *tile = list + (int64_t)at * kListTile;
+  // places without a token: their keys and values are zero, their scores start from -infinity
+  uint64_t drop = x.drop;
+  if (v >= c0 && v < nblk) drop = 0;  // residual tokens are put in their places
+  if (v >= nblk) {
+    const int r = (v - nblk) * P + lane;
+    const bool later = r < p.nres && p.res_idx[u * p.nres_cap + r] >= c0 * P;
+    drop |= __ballot(later);
+  }
+  if (is_int_level(x.level)) {
+    if (pg == 0) store_head(lds, load_head(x, lane), lane, p.vtok);
+    __syncthreads();
+  }
+  Raw k, w;
+  uint32_t y[16];
+  load_raw<GKV_KEYS>(k, x.k, x.level, pg, lane);
+  load_raw<GKV_VALUES>(w, x.v, x.level, pg, lane);
+  key_words_any(y, k, x.level, lds, kg);
+  if (drop >> (16 * pg + m) & 1)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *(u4 *)(tile + ta::key_place(16 * pg + m, 4 * j + kg)) = u4{y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]};
+  Visit xd = x;
+  xd.drop = drop;
+  value_words_any(y, w, xd, lds, pg, lane, p.vtok);
+  // operand form; two lanes' halves of a unit are exchanged, so that each stores 16 bytes: a lane
+  // of the lower groups the units of even channel groups, its partner those of odd ones
+  uint8_t *to = tile + ta::kTileBytes + pg * 4096 + (kg & 1) * 512 + m * 16;
+#pragma unroll
+  for (int c = 0; c < 8; c += 2) {
+    const bool low = kg < 2;
+    uint32_t mine[2], other[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t give = low ? y[2 * (c + 1) + i] : y[2 * c + i];
+      mine[i] = low ? y[2 * c + i] : y[2 * (c + 1) + i];
+      other[i] = __shfl_xor(give, 32);
+    }
+    const int cc = low ? c : c + 1;
+    *(u4 *)(to + (cc >> 1) * 1024 + (cc & 1) * 256) =
+        low ? u4{mine[0], mine[1], other[0], other[1]} : u4{other[0], other[1], mine[0], mine[1]};
+  }
+  if (pg == 0) ((float *)(tile + 2 * ta::kTileBytes))[lane] = drop >> lane & 1 ? -__builtin_inff() : 0.f;
+  if (v >= c0 && v < nblk && x.drop) {  // the residual tokens' exact rows
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the graded ones are written
+    __syncthreads();
+    const int32_t *off = p.res_off + u * (p.nblk_cap + 1) + v;
+    for (int t = tid >> 4; t < P; t += 16) {
+      if (!(x.drop >> t & 1)) continue;
+      const int r = off[0] + __popcll(x.drop & ((1ull << t) - 1));
+      const uint8_t *rec = p.res_rows + (u * p.nrb_cap + (r >> 6)) * (2 * kExactBytes);
+      const int rt = r & 63, un = tid & 15;
+      *(u4 *)(tile + ta::key_place(t, un)) =
+          *(const u4 *)(rec + (((rt >> 4) * 64 + (un & 3) * 16 + (rt & 15)) * 4 + (un >> 2)) * 16);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {  // channels 8 un + i
+        const int d = 8 * un + i;
+        const int src = ((rt >> 4) * 64 + ((rt >> 2) & 3) * 16 + (d & 15)) * 32 + (d >> 4) * 4 + (rt & 3);
+        const int dst = ((t >> 4) * 4 + (d >> 5)) * 1024 + 512 * ((t >> 2) & 1) + 16 * (d & 31) + 8 * ((t >> 3) & 1) + 2 * (t & 3);
+        *(uint16_t *)(tile + ta::kTileBytes + dst) = ((const uint16_t *)(rec + kExactBytes))[src];
+      }
+    }
+  }
+}
+
+// A list's tiles: 1 KB a copy.
 template <int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 2) chunk_kernel(const ChunkParams p) {
+struct ListTiles {
+  const uint8_t *list;
+  int wave, lane;
+  __device__ __forceinline__ void copy(const uint8_t *src, uint32_t lds) const {
+#pragma unroll
+    for (int i = 0; i < 16 / WAVES; ++i) {
+      const uint32_t at = (wave + WAVES * i) * 1024;
+      ta::dma16(lane * 16, src + at, lds + at);
+    }
+  }
+  __device__ __forceinline__ void keys(int t, uint32_t lds, uint32_t bias) const {
+    const uint8_t *tile = list + (int64_t)t * kListTile;
+    copy(tile, lds);
+    if (wave == 0 && lane < 16) ta::dma16(lane * 16, tile + 2 * ta::kTileBytes, bias);
+  }
+  __device__ __forceinline__ void values(int t, uint32_t lds) const {
+    copy(list + (int64_t)t * kListTile + ta::kTileBytes, lds);
+  }
+};
+
+template <int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams p) {
   extern __shared__ __align__(16) unsigned char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
   constexpr int kTileRows = 32 * WAVES;
@@ -380,112 +574,460 @@ __global__ void __launch_bounds__(64 * WAVES, 2) chunk_kernel(const ChunkParams 
   const int row = j.tile * kTileRows + 32 * wave + ln.col;
   const int rc = row < j.rows ? row : j.rows - 1;  // rows past the last are copies, not stored
   const int tok = rc / p.G, g = rc - tok * p.G;
-  u4 q[8];
-  load_queries(q, p, j, tok, g, ln.hf);
-#pragma unroll
-  for (int d = 0; d < 8; ++d) asm volatile("" : "+v"(q[d]));
-
   const int first = j.pos0 + (j.tile * kTileRows) / p.G;  // seen by every row up to here
   const int last = j.pos0 + min(j.tile * kTileRows + kTileRows - 1, j.rows - 1) / p.G;
-  const int nblk = last / P + 1;  // blocks that some row sees
-  const int nvis = nblk + (p.nres + P - 1) / P;
+  const int c0 = j.pos0 / P, whole = (int)table32(p.whole, j.s * p.Hkv + j.h);
+  const int ntile = whole + last / P - c0 + 1;
+  const int split = p.split[j.s];
+  const int t0 = (int)((int64_t)ntile * j.part / split), t1 = (int)((int64_t)ntile * (j.part + 1) / split);
+  const ListTiles<WAVES> src = {p.list + (p.list0[j.s] + (int64_t)j.h * list_tiles(p, j.T)) * kListTile, wave, ln.lane};
+  ta::Rows st;
+  u4 q[8];
+  st.init();
+  if (t0 < t1)  // (a row tile with fewer tiles than shares leaves some of them none)
+    ta::attend<T16, WAVES, false, true>(
+        st, ln, q, lds, wave, t0, t1, whole + (first + 1) / P - c0, p.sl2, src,
+        [&](int t) {  // this row's visible tokens of tile t
+          const int n = t < whole ? P : j.pos0 + tok + 1 - (c0 + t - whole) * P;
+          return n >= P ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
+        },
+        [&] { load_queries(q, p, j, tok, g, ln.hf); });
+  const float l = st.l + ta::other_half(st.l);
+  if (row >= j.rows) return;
+  if (split == 1) store_row(p, j, tok, g, st, l > 0.f ? 1.f / l : l, ln.hf);
+  else store_part(p.part + (part_row(p, j, kTileRows) + 32 * wave + ln.col) * kPart, st, l, ln.hf);
+}
+
+// ---------------------------------------------------------------- few rows
+// At most 16 CT rows of a (sequence, KV head): every wavefront holds all of them and reads whole
+// blocks of its own, straight from the records into operands.  The records are laid out for
+// 16x16x32 MFMA (a lane's key chunk is the four operands of its page, its value chunk of two
+// pages the eight operands of 32 tokens), so nothing passes through LDS but the integer
+// levels' scales.  Scores are formed for 64 tokens, in the layout (lane l: row l & 15, token
+// 16 page + 4 (l >> 4) + i) that is the second product's operand layout again.  Bound by the
+// records' bytes and, near it, by the vector instructions that decode them (3.5 a pair).
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+template <int CT>
+struct FewRows {
+  f4 o[8][CT];  // O^T: register i of group c is channel 16 c + 4 kg + i
+  float m[CT], raise[CT], l[CT];
+};
+
+__device__ __forceinline__ f4 mfma16(u4 a, u4 b, f4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta::half8, a), __builtin_bit_cast(ta::half8, b), c,
+                                                0, 0, 0);
+}
+
+__device__ __forceinline__ float over_groups(float x) {  // the maximum over a row's four lanes
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// Scores to packed probabilities (two dwords a page), raising the maxima as tile_attn.h does.
+template <int CT, int NP>
+__device__ __forceinline__ void few_weights(uint32_t (&p)[CT][2 * NP], FewRows<CT> &r, const f4 (&s)[NP][CT],
+                                            float sl2) {
+  float top[CT];
+  bool go = false;
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+    top[t] = -__builtin_inff();
+#pragma unroll
+    for (int g = 0; g < NP; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], __builtin_fmaf(s[g][t][i], sl2, -r.m[t]));
+    go |= top[t] > r.raise[t];
+  }
+  if (__builtin_expect(__any(go), 0)) {
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      const float high = over_groups(top[t]);
+      const bool mine = high > r.raise[t];
+      const float up = mine ? high : 0.f;
+      const float f = r.raise[t] < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
+      r.raise[t] = mine ? ta::kRescale : r.raise[t];
+      r.m[t] += up;
+      r.l[t] *= f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.o[c][t][i] *= f;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int g = 0; g < NP; ++g)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][t][2 * i], sl2, -r.m[t]));
+        const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][t][2 * i + 1], sl2, -r.m[t]));
+        const uint32_t w = T16::pack(a, b);
+        p[t][2 * g + i] = w;
+        r.l[t] = T16::add2(w, r.l[t]);
+      }
+}
+
+// Scores of page g (keys as 16 words a lane).
+template <int CT>
+__device__ __forceinline__ void few_scores(f4 (&s)[CT], const uint32_t (&y)[16], const u4 (&q)[4][CT]) {
+#pragma unroll
+  for (int t = 0; t < CT; ++t) s[t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+      s[t] = mfma16(u4{y[4 * d], y[4 * d + 1], y[4 * d + 2], y[4 * d + 3]}, q[d][t], s[t]);
+}
+template <int CT>
+__device__ __forceinline__ void few_mask(f4 (&s)[4][CT], const uint64_t (&vis)[CT], int kg) {
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+    const uint64_t w = vis[t] >> (4 * kg);
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[g][t][i] = w >> (16 * g + i) & 1 ? s[g][t][i] : -__builtin_inff();
+  }
+}
+// The value product of pages 2 pp and 2 pp + 1.
+template <int CT>
+__device__ __forceinline__ void few_outputs(FewRows<CT> &r, const uint32_t (&y)[2][16], const uint32_t (&w)[CT][8],
+                                            int pp) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+      r.o[c][t] = mfma16(u4{y[0][2 * c], y[0][2 * c + 1], y[1][2 * c], y[1][2 * c + 1]},
+                         u4{w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]}, r.o[c][t]);
+}
+
+// The first 64 bytes a lane needs of a record's codes or rows, as four 16-byte loads whose
+// addresses alone go by the level (int4: all four pages; int8: two; int2: four, half of each
+// load another lane's; exact: one; one-centroid keys: the row): so they can be in flight
+// across the branches that the levels take.
+__device__ __forceinline__ void load_ahead(u4 (&y)[4], const uint8_t *rec, int level, int lane) {
+  const uint8_t *at = rec + (level == GKV_EXACT ? lane * 64
+                             : level == GKV_INT8 ? kSZBytes + lane * 32
+                             : level == GKV_INT4 ? kSZBytes + lane * 16
+                             : level == GKV_INT2 ? kSZBytes + (lane & ~1) * 8
+                                                 : (lane >> 4) * 16);
+  const int s1 = level == GKV_INT4 ? 1024 : level == GKV_INT2 ? 512 : level == GKV_MEAN || level == GKV_CENTROID ? 64 : 16;
+  const int s2 = level == GKV_INT8 ? 2048 : 2 * s1;
+  y[0] = *(const u4 *)at;
+  y[1] = *(const u4 *)(at + s1);
+  y[2] = *(const u4 *)(at + s2);
+  y[3] = *(const u4 *)(at + s1 + s2);
+}
+// A lane's chunk of page g: from what was loaded ahead, or loaded now.
+template <int TENSOR, int LEVEL>
+__device__ __forceinline__ void take(Raw &x, const u4 (&y)[4], const uint8_t *rec, int g, int lane) {
+  if constexpr (LEVEL == GKV_INT4) {
+    x.w[0] = y[g];
+  } else if constexpr (LEVEL == GKV_INT2) {
+    x.w[0][0] = lane & 1 ? y[g][2] : y[g][0];
+    x.w[0][1] = lane & 1 ? y[g][3] : y[g][1];
+  } else if (LEVEL == GKV_INT8 && g < 2) {
+    x.w[0] = y[2 * g];
+    x.w[1] = y[2 * g + 1];
+  } else if ((LEVEL == GKV_EXACT && g == 0) || (LEVEL == GKV_MEAN && TENSOR == GKV_KEYS)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.w[i] = y[i];
+  } else {
+    load_raw<TENSOR>(x, rec, LEVEL, g, lane);
+  }
+}
+
+// A block that every row sees whole, but for the tokens in x.drop: its scores ...
+template <int LEVEL, int CT>
+__device__ __forceinline__ void few_keys(f4 (&s)[4][CT], const Visit &x, const u4 (&ahead)[4], const u4 (&q)[4][CT],
+                                         float sl2, uint32_t head, int lane) {
+  const int kg = lane >> 4;
+  uint32_t y[16];
+  if constexpr (LEVEL == GKV_MEAN) {
+    // one key stands for all the block's tokens: its weight times their number, in the first
+    // group's first place alone
+    Raw k;
+    take<GKV_KEYS, LEVEL>(k, ahead, x.k, 0, lane);
+    key_words<LEVEL>(y, k, head, kg);
+    few_scores<CT>(s[0], y, q);
+    const int n = P - __popcll(x.drop);
+    const float more = __builtin_amdgcn_logf((float)n) / sl2, no = -__builtin_inff();
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[g][t][i] = g == 0 && i == 0 && kg == 0 && n ? s[0][t][0] + more : no;
+  } else {
+    Raw k[4];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) take<GKV_KEYS, LEVEL>(k[g], ahead, x.k, g, lane);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g + 2 < 4) take<GKV_KEYS, LEVEL>(k[g + 2], ahead, x.k, g + 2, lane);
+      key_words<LEVEL>(y, k[g], head, kg);
+      few_scores<CT>(s[g], y, q);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+// ... and, with their weights, its outputs.
+template <int LEVEL, int CT>
+__device__ __forceinline__ void few_values(FewRows<CT> &r, const uint32_t (&w)[CT][8], const Visit &x,
+                                           const u4 (&ahead)[4], bool vtok, uint32_t head, int lane) {
+  if constexpr (LEVEL == GKV_MEAN) {
+    Raw v;
+    load_raw<GKV_VALUES>(v, x.v, LEVEL, 0, lane);
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+        r.o[c][t] = mfma16(u4{v.w[c >> 2][c & 3] & 0xFFFFu, 0, 0, 0}, u4{w[t][0], 0, 0, 0}, r.o[c][t]);
+  } else {
+    Raw v[4];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) take<GKV_VALUES, LEVEL>(v[g], ahead, x.v, g, lane);
+#pragma unroll
+    for (int pp = 0; pp < 2; ++pp) {
+      uint32_t y[2][16];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        value_words<LEVEL>(y[g], v[2 * pp + g], x.v, x.drop, head, 2 * pp + g, lane, vtok);
+        if (!pp) take<GKV_VALUES, LEVEL>(v[2 + g], ahead, x.v, 2 + g, lane);
+      }
+      few_outputs<CT>(r, y, w, pp);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+// A block that some row sees in part (the last ones of a sequence), of any level: its keys, then
+// its values pass through LDS (16 KB at buf), where infinities and NaN among the values
+// are found, kept out of the product and noted for the rows that see them (two bits an
+// output, as in find_odd).
+template <int CT>
+__device__ __forceinline__ void few_part(FewRows<CT> &r, const ChunkParams &p, const Visit &x, const u4 (&q)[4][CT],
+                                         const uint64_t (&vis)[CT], u4 (&odd)[CT], uint32_t head, uint32_t buf, int lane) {
+  const int kg = lane >> 4;
+  auto put = [&](const uint32_t (&y)[16], int g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(LdsW4)(uintptr_t)(buf + g * 4096 + i * 1024 + lane * 16) = u4{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]};
+  };
+  auto get = [&](uint32_t (&y)[16], int g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u4 a = ta::lds_u4(buf + g * 4096 + i * 1024 + lane * 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[4 * i + k] = a[k];
+    }
+  };
+#pragma unroll 1
+  for (int g = 0; g < 4; ++g) {
+    Raw k;
+    uint32_t y[16];
+    load_raw<GKV_KEYS>(k, x.k, x.level, g, lane);
+    key_words_any(y, k, x.level, head, kg);
+    put(y, g);
+  }
+  f4 s[4][CT];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    uint32_t y[16];
+    get(y, g);
+    few_scores<CT>(s[g], y, q);
+  }
+  few_mask<CT>(s, vis, kg);
+  uint32_t w[CT][8];
+  few_weights<CT, 4>(w, r, s, p.sl2);
+  float zero = 0.f;
+#pragma unroll 1
+  for (int g = 0; g < 4; ++g) {
+    Raw v;
+    uint32_t y[16];
+    load_raw<GKV_VALUES>(v, x.v, x.level, g, lane);
+    value_words_any(y, v, x, head, g, lane, p.vtok);
+    put(y, g);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero = T16::times0(y[i], zero);
+  }
+  if (__builtin_expect(__any(zero != zero), 0)) {
+    // output (c, i) of a lane is channel 16 c + 4 kg + i; token 4 a + b of a page lies in
+    // lane 16 a + 4 kg + i's words 2 c, 2 c + 1 at half b
+#pragma unroll 1
+    for (int tok = 0; tok < P; ++tok) {
+      const uint32_t at = buf + (tok >> 4) * 4096 + (16 * (tok >> 2 & 3) + 4 * kg) * 16 + 2 * (tok & 3);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t h = *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)(
+              at + (c >> 1) * 1024 + (c & 1) * 8 + i * 16);
+          const uint32_t e = h & 0x7FFFu, b = e < T16::kInf ? 0u : e > T16::kInf ? 3u : h == e ? 1u : 2u;
+#pragma unroll
+          for (int t = 0; t < CT; ++t) odd[t][c >> 1] |= (vis[t] >> tok & 1 ? b : 0u) << (8 * (c & 1) + 2 * i);
+        }
+    }
+#pragma unroll 1
+    for (int g = 0; g < 4; ++g) {
+      uint32_t y[16];
+      get(y, g);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] &= ~ta::bad_halves<T16>(y[i]);
+      put(y, g);
+    }
+  }
+#pragma unroll
+  for (int pp = 0; pp < 2; ++pp)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u4 a = ta::lds_u4(buf + 2 * pp * 4096 + i * 1024 + lane * 16);
+      const u4 b = ta::lds_u4(buf + (2 * pp + 1) * 4096 + i * 1024 + lane * 16);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+          r.o[2 * i + k][t] = mfma16(u4{a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1]},
+                                     u4{w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]},
+                                     r.o[2 * i + k][t]);
+    }
+}
+
+constexpr int kFewWaves = 4;
+constexpr int kFewRow = D + 4;             // floats of a row in the wavefronts' merge
+
+template <int CT>
+__global__ void __launch_bounds__(64 * kFewWaves, CT == 1 ? 2 : 1) few_kernel(const ChunkParams p) {
+  constexpr int kR = 16 * CT;
+  // a wavefront's part: a header and a block's keys or values, then its state
+  constexpr int kFewLds = 1024 + kRecTile > kR * kFewRow * 4 ? 1024 + kRecTile : kR * kFewRow * 4;
+  __shared__ __align__(16) float sh[kFewWaves * kFewLds / 4];
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)sh;
+  const Job j = job_of(p, kR);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int kg = lane >> 4, m = lane & 15;
+  int tok[CT], g[CT];
+  u4 q[4][CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+    const int rc = min(16 * t + m, j.rows - 1);  // rows past the last are copies, not stored
+    tok[t] = rc / p.G;
+    g[t] = rc - tok[t] * p.G;
+    const uint16_t *qp = p.q + (j.row0 + tok[t]) * p.qs + (int64_t)(j.h * p.G + g[t]) * D + 8 * kg;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) q[d][t] = *(const u4 *)(qp + 32 * d);
+  }
+  FewRows<CT> r;
+  u4 odd[CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) r.o[c][t] = f4{0.f, 0.f, 0.f, 0.f};
+    r.m[t] = r.l[t] = 0.f;
+    r.raise[t] = -__builtin_inff();
+    odd[t] = u4{0, 0, 0, 0};
+  }
+  const int nvis = j.nblk + (p.nres + P - 1) / P;
   const int split = p.split[j.s];
   const int v0 = (int)((int64_t)nvis * j.part / split), v1 = (int)((int64_t)nvis * (j.part + 1) / split);
-  auto visit = [&](int v) { return visit_at(p, j.u, v < nblk ? v : j.nblk + v - nblk, j.nblk); };
-
-  const uint32_t head = lds + 4 * kRecTile;
-  auto tiles = [&](int v) { return lds + (v & 1) * 2 * kRecTile; };
-  constexpr bool kBoth = WAVES == 4;  // a wavefront stages a page of both tensors, or of one
-  const int pg = wave & 3;
-  const bool key_wave = wave < 4;
-  Raw raw[kBoth ? 2 : 1];
-  u4 hd;
-  auto load = [&](const Visit &x) {
-    if (kBoth) {
-      load_raw<GKV_KEYS>(raw[0], x.k, x.level, pg, ln.lane);
-      load_raw<GKV_VALUES>(raw[kBoth], x.v, x.level, pg, ln.lane);
-    } else if (key_wave) {
-      load_raw<GKV_KEYS>(raw[0], x.k, x.level, pg, ln.lane);
-    } else {
-      load_raw<GKV_VALUES>(raw[0], x.v, x.level, pg, ln.lane);
-    }
+  const uint32_t head = lds + wave * kFewLds;
+  int v = v0 + wave;
+  Visit x;
+  u4 ka[4], va[4], hd = {0, 0, 0, 0};
+  auto ahead = [&] {
+    if (is_int_level(x.level)) hd = load_head(x, lane);
+    load_ahead(ka, x.k, x.level, lane);
   };
-  auto stage = [&](const Visit &x, int v) {
-    const uint32_t to = tiles(v), hv = head + (v & 1) * 1024;
-    if (kBoth || key_wave) stage_keys(raw[0], x.level, hv, to, pg, ln.lane);
-    if (kBoth || !key_wave)
-      stage_values(raw[kBoth], x.level, x.v, x.drop, hv, to + kRecTile, pg, pg, ln.lane, p.vtok);
-  };
-  auto meet = [] {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  // Tile v is staged, and the header of v + 1 lies in LDS, when its turn comes; the codes of
-  // v + 1 and the header of v + 2 are in registers, the tables of v + 2 read.
-  ta::Rows st;
-  st.init();
-  u4 odd = {0, 0, 0, 0};
-  if (v0 < v1) {  // (a tile that sees few blocks may leave some of its workgroups nothing)
-    auto fetch_head = [&](const Visit &x) {
-      if (wave == 0 && is_int_level(x.level)) hd = load_head(x, ln.lane);
-    };
-    auto put_head = [&](const Visit &x, int v) {
-      if (wave == 0 && is_int_level(x.level)) store_head(head + (v & 1) * 1024, hd, ln.lane, p.vtok);
-    };
-    Visit x0 = visit(v0), x1 = v0 + 1 < v1 ? visit(v0 + 1) : x0, x2 = v0 + 2 < v1 ? visit(v0 + 2) : x1;
-    load(x0);
-    fetch_head(x0);
-    put_head(x0, v0);
-    meet();
-    stage(x0, v0);
-    load(x1);
-    fetch_head(x1);
-    put_head(x1, v0 + 1);
-    fetch_head(x2);
-    for (int v = v0; v < v1; ++v) {
-      meet();
-      if (v + 1 < v1) {
-        stage(x1, v + 1);
-        put_head(x2, v);
-        load(x2);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      f16v s[2];
-      u4 pr[4];
-      ta::scores<T16, 2>(s, ln, q, tiles(v));
-      const int vv = v < nblk ? v : j.nblk + v - nblk;
-      const bool whole = whole_at(p, j, vv, first);
-      uint64_t vis = ~0ull;
-      if (!whole || x0.drop) {
-        vis = seen_by(p, j, vv, x0.drop, j.pos0 + tok);
-        ta::mask_scores<2>(s, ln, vis);
-      }
-      x0 = x1;
-      x1 = x2;
-      if (v + 3 < v1) x2 = visit(v + 3);
-      fetch_head(x2);
-      ta::weights<T16, 2>(pr, st, s, p.sl2);
-      const uint32_t values = tiles(v) + kRecTile;
-      if (!whole && ta::find_odd<T16, 2, false>(ln, values, vis, odd)) {  // alike for all wavefronts
-        meet();  // each has found them
-        for (int i = threadIdx.x; i < kRecTile / 16; i += 64 * WAVES) {
-          u4 y = ta::lds_u4(values + 16 * i);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) y[k] &= ~ta::bad_halves<T16>(y[k]);
-          *(LdsW4)(uintptr_t)(values + 16 * i) = y;
-        }
-        meet();
-      }
-      ta::outputs<T16, 2, false>(st, ln, pr, values);
-    }
-    ta::add_odd(st, odd);
+  if (v < v1) {
+    x = visit_at(p, j.u, v, j.nblk);
+    ahead();
   }
-  const float l = st.l + ta::other_half(st.l);
-  if (split == 1) {
-    if (row < j.rows) store_row(p, j, tok, g, st, l > 0.f ? 1.f / l : l, ln.hf);
-  } else if (row < j.rows) {
-    store_part(p.part + (part_row(p, j, kTileRows) + 32 * wave + ln.col) * kPart, st, l, ln.hf);
+  while (v < v1) {
+    const Visit now = x;
+    const int at = v;
+    v += kFewWaves;
+    if (v < v1) x = visit_at(p, j.u, v, j.nblk);
+    if (is_int_level(now.level)) store_head(head, hd, lane, p.vtok);
+    if (!whole_at(p, j, at, j.pos0)) {
+      uint64_t vis[CT];
+#pragma unroll
+      for (int t = 0; t < CT; ++t) vis[t] = seen_by(p, j, at, now.drop, j.pos0 + tok[t]);
+      few_part<CT>(r, p, now, q, vis, odd, head, head + 1024, lane);
+      ahead();
+      continue;
+    }
+    load_ahead(va, now.v, now.level, lane);
+    f4 s[4][CT];
+#define GKV_LEVELS(f, ...)                                             \
+  if (now.level == GKV_INT4) f<GKV_INT4, CT>(__VA_ARGS__);             \
+  else if (now.level == GKV_INT2) f<GKV_INT2, CT>(__VA_ARGS__);        \
+  else if (now.level == GKV_INT8) f<GKV_INT8, CT>(__VA_ARGS__);        \
+  else if (now.level == GKV_EXACT) f<GKV_EXACT, CT>(__VA_ARGS__);      \
+  else if (now.level == GKV_CENTROID) f<GKV_CENTROID, CT>(__VA_ARGS__); \
+  else f<GKV_MEAN, CT>(__VA_ARGS__)
+    GKV_LEVELS(few_keys, s, now, ka, q, p.sl2, head, lane);
+    ahead();
+    if (now.drop && now.level != GKV_MEAN) {
+      uint64_t vis[CT];
+#pragma unroll
+      for (int t = 0; t < CT; ++t) vis[t] = ~now.drop;
+      few_mask<CT>(s, vis, kg);
+    }
+    uint32_t w[CT][8];
+    few_weights<CT, 4>(w, r, s, p.sl2);
+    GKV_LEVELS(few_values, r, w, now, va, p.vtok, head, lane);
+#undef GKV_LEVELS
+  }
+  // the wavefronts' states, joined in LDS
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+    float l = r.l[t];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {  // the values that stayed out of the products
+      const uint32_t b = odd[t][i >> 3] >> (8 * (i >> 2 & 1) + 2 * (i & 3)) & 3u;
+      r.o[i >> 2][t][i & 3] += b == 0 ? 0.f : b == 3 ? __builtin_nanf("") : b == 1 ? __builtin_inff() : -__builtin_inff();
+    }
+    float *row = sh + wave * (kFewLds / 4) + (16 * t + m) * kFewRow;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) *(f4 *)(row + 16 * c + 4 * kg) = r.o[c][t];
+    if (kg == 0) {
+      row[D] = r.m[t];
+      row[D + 1] = l;
+    }
+  }
+  __syncthreads();
+  for (int i = wave; i < min(kR, j.rows); i += kFewWaves) {  // a row a wavefront, two channels a lane
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < kFewWaves; ++k) {
+      const float *row = sh + k * (kFewLds / 4) + i * kFewRow;
+      if (row[D + 1] != 0.f) top = fmaxf(top, row[D]);
+    }
+    float a = 0.f, b = 0.f, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kFewWaves; ++k) {
+      const float *row = sh + k * (kFewLds / 4) + i * kFewRow;
+      if (row[D + 1] == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(row[D] - top);
+      a += f * row[2 * lane];
+      b += f * row[2 * lane + 1];
+      l += f * row[D + 1];
+    }
+    if (split == 1) {
+      const float inv = l > 0.f ? 1.f / l : l;
+      const int tk = i / p.G, gg = i - tk * p.G;
+      *(uint32_t *)(p.out + (j.row0 + tk) * p.os + (int64_t)(j.h * p.G + gg) * D + 2 * lane) =
+          T16::pack(a * inv, b * inv);
+    } else {
+      float *part = p.part + (part_row(p, j, kR) + i) * kPart;
+      *(float2 *)(part + 2 * lane) = make_float2(a, b);
+      if (lane == 0) *(float2 *)(part + D) = make_float2(top == -__builtin_inff() ? 0.f : top, l);
+    }
   }
 }
 
@@ -506,17 +1048,19 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, i
   const int tok = (int)r / p.G, g = (int)r - tok * p.G;
   const float *part = p.part + (p.part0 + ((int64_t)h * p.wg0[p.nseq] + p.wg0[s] + tile) * rows_tile + in) * kPart;
   const int64_t step = (int64_t)tiles * rows_tile * kPart;
+  const int n = p.split[s];
   float m = -__builtin_inff();
-  for (int i = 0; i < p.split[s]; ++i) {
+  for (int i = lane; i < n; i += 64) {
     const float2 ml = *(const float2 *)(part + i * step + D);
     if (ml.y != 0.f) m = fmaxf(m, ml.x);  // (one that saw nothing has no maximum)
   }
+#pragma unroll
+  for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
   float a = 0.f, b = 0.f, l = 0.f;
-  for (int i = 0; i < p.split[s]; ++i) {
-    const float2 ml = *(const float2 *)(part + i * step + D);
-    if (ml.y == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-    const float2 o = *(const float2 *)(part + i * step + 2 * lane);
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    const float2 ml = *(const float2 *)(part + i * step + D), o = *(const float2 *)(part + i * step + 2 * lane);
+    const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
     a += f * o.x;
     b += f * o.y;
     l += f * ml.y;
@@ -526,21 +1070,59 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, i
 }
 
 // ---------------------------------------------------------------- host
-struct Plan {
+// Rows of a (sequence, KV head) up to which its blocks are read by few_kernel, decoded for every
+// wavefront's rows anew; beyond, the cache is decoded to tiles first, which costs its
+// bytes written and read again (0.26 ns a token of a KV head, as much as 512 rows' products).
+constexpr int kFewMost = 64;
+constexpr int kLeastVisits = 4;  // blocks that a workgroup takes at least
+constexpr int64_t kCus = 256;
+
+// One launch's part of a call.
+struct Part {
+  ChunkParams p;
   int rows_tile;
-  int64_t wgs, part_rows;  // workgroups per KV head; partial rows over all KV heads
+  int64_t wgs, merged, part_rows, tiles;  // workgroups per KV head, rows to merge per KV head, partial
+                                          // rows and list tiles over all KV heads
 };
 
-}  // namespace
-
-// Visits a workgroup takes at least, and the workgroups that fill the chip.
-constexpr int kLeastVisits = 4;
-constexpr int64_t kFill = 256;
-
-static gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, ChunkParams &p, Plan &pl) {
-  p.nseq = 0;
+gkv_status plan_part(Part &t, const gkv_cache *c, int64_t fill) {
+  ChunkParams &p = t.p;
   const int G = c->Hq / c->Hkv;
-  int64_t rows = 0, visits = 0, most = 0;
+  auto tiles = [&](int i) { return ((int64_t)p.n[i] * G + t.rows_tile - 1) / t.rows_tile; };
+  int64_t total = 0, plain = 0;
+  t.wgs = t.merged = t.part_rows = t.tiles = 0;
+  for (int i = 0; i < p.nseq; ++i) {
+    total += tiles(i) * list_tiles(p.T[i], c->nres) * c->Hkv;
+    plain += tiles(i) * c->Hkv;
+  }
+  // as many workgroups as are resident at once; no split where the row tiles alone are
+  int64_t per = plain >= fill ? 0x7fffffff : (total + fill - 1) / fill;
+  if (per < kLeastVisits) per = kLeastVisits;
+  for (int i = 0; i < p.nseq; ++i) {
+    int64_t s = list_tiles(p.T[i], c->nres) / per;
+    s = s < 1 ? 1 : s > 0xffff ? 0xffff : s;
+    p.split[i] = (uint16_t)s;
+    p.wg0[i] = (int32_t)t.wgs;
+    p.list0[i] = (int32_t)t.tiles;
+    if (s > 1) t.merged += (int64_t)p.n[i] * G;
+    t.wgs += s * tiles(i);
+    t.tiles += (int64_t)list_tiles(p.T[i], c->nres) * c->Hkv;
+    if (t.wgs * c->Hkv > 0x7fffffff || t.tiles > 0x7fffffff) return GKV_E_UNSUPPORTED;
+  }
+  p.wg0[p.nseq] = (int32_t)t.wgs;
+  t.part_rows = t.merged ? t.wgs * c->Hkv * t.rows_tile : 0;
+  return GKV_OK;
+}
+
+struct Plan {
+  Part few, many;
+  int64_t part, whole, list, bytes;  // workspace: partials | whole counts | lists
+};
+
+gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
+  const int G = c->Hq / c->Hkv;
+  pl.few.p.nseq = pl.many.p.nseq = 0;
+  int64_t rows = 0, most = 0;
   for (int b = 0; b < c->B; ++b) {
     const int64_t T = seq_tokens(c, b), n = n_new[b];
     if (n < 0) return GKV_E_SHAPE;
@@ -548,47 +1130,46 @@ static gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, ChunkPara
     if (T < 0) return GKV_E_ARG;
     if (n > T) return GKV_E_SHAPE;
     if (T > 0x7fffff00 || n * G > 0x7fffff00 || rows + n > 0x7fffffff) return GKV_E_UNSUPPORTED;
+    const bool few = n * G <= kFewMost;
+    ChunkParams &p = few ? pl.few.p : pl.many.p;
     const int i = p.nseq++;
-    p.seq[i] = b;
+    p.seq[i] = (uint8_t)b;
     p.T[i] = (int32_t)T;
     p.n[i] = (int32_t)n;
     p.row0[i] = (int32_t)rows;
     rows += n;
-    most = n * G > most ? n * G : most;
+    if (few && n * G > most) most = n * G;
   }
-  pl.rows_tile = most <= 128 ? 128 : 256;
-  auto vis = [&](int i) { return (p.T[i] + P - 1) / P + (c->nres + P - 1) / P; };
-  auto tiles = [&](int i) { return ((int64_t)p.n[i] * G + pl.rows_tile - 1) / pl.rows_tile; };
-  int64_t total = 0, plain = 0;
-  for (int i = 0; i < p.nseq; ++i) {
-    total += tiles(i) * vis(i) * c->Hkv;
-    plain += tiles(i) * c->Hkv;
-  }
-  const int64_t fill = pl.rows_tile == 128 ? 2 * kFill : kFill;
-  int64_t per = plain >= fill ? 0x7fffffff : (total + fill - 1) / fill;  // visits a workgroup
-  if (per < kLeastVisits) per = kLeastVisits;
-  pl.wgs = 0;
-  bool any = false;
-  for (int i = 0; i < p.nseq; ++i) {
-    int64_t s = vis(i) / per;
-    s = s < 1 ? 1 : s;
-    p.split[i] = (int32_t)s;
-    p.wg0[i] = (int32_t)pl.wgs;
-    any |= s > 1;
-    pl.wgs += s * tiles(i);
-    if (pl.wgs * c->Hkv > 0x7fffffff) return GKV_E_UNSUPPORTED;
-  }
-  p.wg0[p.nseq] = (int32_t)pl.wgs;
-  pl.part_rows = any ? pl.wgs * c->Hkv * pl.rows_tile : 0;
+  pl.few.rows_tile = (int)((most + 15) / 16 * 16);
+  pl.many.rows_tile = 256;
+  gkv_status st = plan_part(pl.few, c, pl.few.rows_tile <= 16 ? 2 * kCus : kCus);
+  if (!st) st = plan_part(pl.many, c, kCus);
+  if (st) return st;
+  auto align = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
+  pl.part = 0;
+  pl.whole = align((pl.few.part_rows + pl.many.part_rows) * kPart * 4);
+  pl.list = align(pl.whole + (int64_t)pl.many.p.nseq * c->Hkv * 4);
+  pl.bytes = pl.list + pl.many.tiles * kListTile;
   return GKV_OK;
 }
 
+void launch_few(const Part &t, const dim3 grid, hipStream_t s) {
+  const dim3 blk(64 * kFewWaves);
+  switch (t.rows_tile) {
+    case 16: hipLaunchKernelGGL((few_kernel<1>), grid, blk, 0, s, t.p); break;
+    case 32: hipLaunchKernelGGL((few_kernel<2>), grid, blk, 0, s, t.p); break;
+    case 48: hipLaunchKernelGGL((few_kernel<3>), grid, blk, 0, s, t.p); break;
+    default: hipLaunchKernelGGL((few_kernel<4>), grid, blk, 0, s, t.p); break;
+  }
+}
+
+}  // namespace
+
 extern "C" int64_t gkv_chunk_ws_bytes(const gkv_cache *c, const int32_t *n_new) {
   if (gkv_validate_cache(c) || !n_new || c->B > kMaxSeqs) return -1;
-  ChunkParams p;
   Plan pl;
-  if (chunk_plan(c, n_new, p, pl)) return -1;
-  return pl.part_rows * kPart * 4;
+  if (chunk_plan(c, n_new, pl)) return -1;
+  return pl.bytes;
 }
 
 extern "C" gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const gkv_cache *c, const int32_t *n_new,
@@ -596,54 +1177,62 @@ extern "C" gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const 
   gkv_status st = gkv_validate_cache(c);
   if (st) return st;
   if (!n_new) return GKV_E_ARG;
-  if (c->B > kMaxSeqs) return GKV_E_UNSUPPORTED;
-  ChunkParams p;
+  if (c->B > kMaxSeqs || c->Hkv > 65535) return GKV_E_UNSUPPORTED;
   Plan pl;
-  st = chunk_plan(c, n_new, p, pl);
+  st = chunk_plan(c, n_new, pl);
   if (st) return st;
-  if (!p.nseq) return GKV_OK;
+  if (!pl.few.p.nseq && !pl.many.p.nseq) return GKV_OK;
   if (!q || !out || (uintptr_t)q % 16 || (uintptr_t)out % 16) return GKV_E_ARG;
   for (const int64_t s : {q_stride, out_stride}) {
     if (s < (int64_t)c->Hq * D) return GKV_E_SHAPE;
     if (s % 8) return GKV_E_ARG;
     if (s > GKV_MAX_ROW_STRIDE) return GKV_E_UNSUPPORTED;
   }
-  if (pl.part_rows && (!ws || (uintptr_t)ws % 16)) return GKV_E_ARG;
-  if (ws_bytes < pl.part_rows * kPart * 4) return GKV_E_WORKSPACE;
-  p.q = q;
-  p.out = out;
-  p.part = (float *)ws;
-  p.qs = q_stride;
-  p.os = out_stride;
-  p.level = c->level;
-  p.koff = c->koff;
-  p.voff = c->voff;
-  p.arena = c->arena;
-  p.res_mask = c->nres ? c->res_mask : nullptr;
-  p.res_idx = c->res_idx;
-  p.res_rows = c->res_rows;
-  p.nblk_cap = c->nblk_cap;
-  p.Hkv = c->Hkv;
-  p.G = c->Hq / c->Hkv;
-  p.nres = c->nres;
-  p.nres_cap = c->nres_cap;
-  p.nrb_cap = (c->nres_cap + P - 1) / P;
-  p.vtok = c->v_per_token;
-  p.sl2 = 1.4426950408889634f / sqrtf((float)D);
-  p.part0 = 0;
+  if (pl.bytes && (!ws || (uintptr_t)ws % 16)) return GKV_E_ARG;
+  if (ws_bytes < pl.bytes) return GKV_E_WORKSPACE;
   const hipStream_t s = (hipStream_t)stream;
-  const dim3 grid((unsigned)(pl.wgs * c->Hkv));
-  constexpr size_t lds = 4 * kRecTile + 2 * 1024;
-  if (pl.rows_tile == 128)
-    hipLaunchKernelGGL((chunk_kernel<4>), grid, dim3(256), lds, s, p);
-  else
-    hipLaunchKernelGGL((chunk_kernel<8>), grid, dim3(512), lds, s, p);
-  if (hipGetLastError() != hipSuccess) return GKV_E_HIP;
-  if (pl.part_rows) {
-    int64_t rows = 0;
-    for (int i = 0; i < p.nseq; ++i) rows += p.split[i] > 1 ? (int64_t)p.n[i] * p.G : 0;
-    hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)((rows + 3) / 4), c->Hkv), dim3(256), 0, s, p, pl.rows_tile);
+  for (Part *t : {&pl.few, &pl.many}) {
+    ChunkParams &p = t->p;
+    if (!p.nseq) continue;
+    p.q = q;
+    p.out = out;
+    p.part = (float *)ws;
+    p.qs = q_stride;
+    p.os = out_stride;
+    p.level = c->level;
+    p.koff = c->koff;
+    p.voff = c->voff;
+    p.arena = c->arena;
+    p.res_mask = c->nres ? c->res_mask : nullptr;
+    p.res_idx = c->res_idx;
+    p.res_off = c->res_off;
+    p.res_rows = c->res_rows;
+    p.nblk_cap = c->nblk_cap;
+    p.Hkv = c->Hkv;
+    p.G = c->Hq / c->Hkv;
+    p.nres = c->nres;
+    p.nres_cap = c->nres_cap;
+    p.nrb_cap = (c->nres_cap + P - 1) / P;
+    p.vtok = c->v_per_token;
+    p.sl2 = 1.4426950408889634f / sqrtf((float)D);
+    p.part0 = t == &pl.few ? 0 : pl.few.part_rows;
+    p.whole = (int32_t *)((uint8_t *)ws + pl.whole);
+    p.list = (uint8_t *)ws + pl.list;
+    const dim3 grid((unsigned)(t->wgs * c->Hkv));
+    if (t == &pl.few) {
+      launch_few(*t, grid, s);
+    } else {
+      int most = 0;
+      for (int i = 0; i < p.nseq; ++i) most = std::max(most, list_tiles(p.T[i], c->nres));
+      hipLaunchKernelGGL(expand_kernel, dim3(most, c->Hkv, p.nseq), dim3(256), 0, s, p);
+      hipLaunchKernelGGL((tiles_kernel<8>), grid, dim3(512), ta::kAttendLds + 2 * ta::kBiasBytes, s, p);
+    }
     if (hipGetLastError() != hipSuccess) return GKV_E_HIP;
+    if (t->merged) {
+      hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)((t->merged + 3) / 4), c->Hkv), dim3(256), 0, s, p,
+                         t->rows_tile);
+      if (hipGetLastError() != hipSuccess) return GKV_E_HIP;
+    }
   }
   return GKV_OK;
 }

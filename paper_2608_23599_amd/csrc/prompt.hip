@@ -9,14 +9,10 @@
 #include "gkv_internal.h"
 #include "tile_attn.h"
 
-#pragma clang diagnostic ignored "-Winline-asm"
-
 using namespace gkv;
 
 namespace {
 
-constexpr int kTile = 64;                   // tokens of a key/value tile
-constexpr int kTileBytes = kTile * D * 2;   // of keys, or of values
 constexpr int kMaxSeqs = GKV_MAX_PROMPTS;
 
 struct PromptParams {
@@ -29,10 +25,26 @@ struct PromptParams {
   int32_t tiles[kMaxSeqs + 1];             // row tiles before each
 };
 
-__device__ __forceinline__ void dma_row(uint32_t voff, const void *base, uint32_t lds) {
-  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(m0v) : "memory", "m0");
-}
+// A prompt's tiles: 4 rows of 256 B a copy, each row's 16-byte units in the places the reads
+// want them in; rows past the end are the last token's again (masked).
+template <int WAVES>
+struct PromptTiles {
+  const uint8_t *k, *v;
+  uint32_t ks, vs;  // bytes from token to token
+  int L, wave, lane;
+  __device__ __forceinline__ void copy(int t, uint32_t lds, const uint8_t *base, uint32_t stride, bool keys) const {
+    const int left = L - 1 - t * ta::kTile;
+    const uint8_t *src = base + (int64_t)t * ta::kTile * stride;
+#pragma unroll
+    for (int i = 0; i < 16 / WAVES; ++i) {
+      const int r4 = 4 * (wave + WAVES * i), r = r4 + (lane >> 4);
+      const int u = (lane & 15) ^ (keys ? r & 15 : (r & 3) << 2);
+      ta::dma16((uint32_t)min(r, left) * stride + (u << 4), src, lds + r4 * 256);
+    }
+  }
+  __device__ __forceinline__ void keys(int t, uint32_t lds, uint32_t) const { copy(t, lds, k, ks, true); }
+  __device__ __forceinline__ void values(int t, uint32_t lds) const { copy(t, lds, v, vs, false); }
+};
 
 template <class T, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParams p) {
@@ -59,110 +71,23 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParam
   const int rc = row < rows ? row : rows - 1;
   const int tok = rc / G, g = rc - tok * G;
   const int first = r0 / G;  // tokens up to this one are seen by every row
-  const int ntile = min(r0 + 32 * WAVES - 1, rows - 1) / G / kTile + 1;
-
-  const uint8_t *kb = (const uint8_t *)(p.k + start * p.ks + (int64_t)h * D);
-  const uint8_t *vb = (const uint8_t *)(p.v + start * p.vs + (int64_t)h * D);
-  // copies: instruction i of this wavefront moves rows 4 (wave + WAVES i) .. + 3 of a tile
-  constexpr int kCopies = 16 / WAVES;
-  const int cr = ln.lane >> 4, cu = ln.lane & 15;
-  auto copy_keys = [&](int t) {
-    const int left = L - 1 - t * kTile;
-    const uint8_t *src = kb + (int64_t)t * kTile * p.ks * 2;
-    const uint32_t buf = lds + (t & 1) * kTileBytes;
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      const int r4 = 4 * (wave + WAVES * i), r = r4 + cr;  // past the end: the last token's row again, masked
-      dma_row((uint32_t)(min(r, left) * (int)p.ks * 2) + ((cu ^ (r & 15)) << 4), src, buf + r4 * 256);
-    }
-  };
-  auto copy_values = [&](int t) {
-    const int left = L - 1 - t * kTile;
-    const uint8_t *src = vb + (int64_t)t * kTile * p.vs * 2;
-    const uint32_t buf = lds + (2 + (t & 1)) * kTileBytes;
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      const int r4 = 4 * (wave + WAVES * i), r = r4 + cr;
-      dma_row((uint32_t)(min(r, left) * (int)p.vs * 2) + ((cu ^ ((r & 3) << 2)) << 4), src, buf + r4 * 256);
-    }
-  };
-  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
-  auto meet = [] {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-
-  copy_keys(0);
-  ta::u4 q[8];
-  {
-    const uint16_t *qp = p.q + (start + tok) * p.qs + (int64_t)(h * G + g) * D + 8 * ln.hf;
-#pragma unroll
-    for (int d = 0; d < 8; ++d) q[d] = *(const ta::u4 *)(qp + 16 * d);
-  }
+  const int ntile = min(r0 + 32 * WAVES - 1, rows - 1) / G / ta::kTile + 1;
+  const PromptTiles<WAVES> src = {(const uint8_t *)(p.k + start * p.ks + (int64_t)h * D),
+                                  (const uint8_t *)(p.v + start * p.vs + (int64_t)h * D),
+                                  (uint32_t)p.ks * 2, (uint32_t)p.vs * 2, L, wave, ln.lane};
   ta::Rows st;
-  st.init();
-  ta::f16v s[2];
-  ta::u4 pr[4];
-  // The two wavefronts of a SIMD work half a tile apart: while one multiplies (the last
-  // tile's values, this tile's keys) the other forms weights.  In the same phase they wait
-  // for one unit together: 43% of the time the MFMAs ran and 49% the vector instructions.
-  const bool second = wave >= WAVES / 2;
-  auto keys = [&](int t) { return lds + (t & 1) * kTileBytes; };
-  auto values = [&](int t) { return lds + (2 + (t & 1)) * kTileBytes; };
-  auto copy = [&](int t) {  // in the interval of the first wavefronts' key product of tile t
-    if (t + 1 < ntile) copy_keys(t + 1);
-    if (t < ntile) copy_values(t);
-  };
-  auto seen = [&](int t) {  // this row's visible tokens of tile t
-    const int n = tok - t * kTile + 1;
-    return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
-  };
-  // Intervals, each ended by a barrier: the first wavefronts' key product of tile t is in
-  // interval 2 t, the second ones' in 2 t + 1.  Keys t + 1 and values t are copied from the
-  // start of interval 2 t on (whose buffers were last read in 2 t - 1) and have arrived at
-  // the end of 2 t + 1.
-  auto before = [&](int t) {  // the value product of tile t
-    if (!second) arrived();
-    meet();
-    if (!second) copy(t + 1);
-  };
-  auto after = [&](int t) {
-    if (second) arrived();
-    meet();
-    if (second) copy(t + 2);
-  };
-  const int full = min(first / kTile, ntile - 1);  // tiles before this one are seen whole by every row
-  arrived();
-  meet();
-  copy(0);
-  if (second) {
-    arrived();
-    meet();
-  }
-  ta::scores<T, 2>(s, ln, q, keys(0));
-  after(-1);
-  int t = 0;
-  for (; t < full; ++t) {
-    ta::weights<T, 2>(pr, st, s, p.sl2);
-    before(t);
-    ta::multiply<T, true>(st, s, ln, pr, q, values(t), keys(t + 1));
-    after(t);
-  }
-  ta::u4 odd = {0, 0, 0, 0};  // infinities and NaN there
-  for (;; ++t) {
-    const uint64_t vis = seen(t);
-    ta::mask_scores<2>(s, ln, vis);
-    ta::weights<T, 2>(pr, st, s, p.sl2);
-    before(t);
-    const bool clean = ta::find_odd<T, 2, true>(ln, values(t), vis, odd);
-    ta::outputs_clean<T, 2, true>(st, ln, pr, values(t), clean);
-    if (t == ntile - 1) break;
-    ta::scores<T, 2>(s, ln, q, keys(t + 1));
-    after(t);
-  }
-  if (!second) meet();
-  ta::add_odd(st, odd);
+  ta::u4 q[8];
+  ta::attend<T, WAVES, true, false>(
+      st, ln, q, lds, wave, 0, ntile, first / ta::kTile, p.sl2, src,
+      [&](int t) {  // this row's visible tokens of tile t
+        const int n = tok - t * ta::kTile + 1;
+        return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
+      },
+      [&] {
+        const uint16_t *qp = p.q + (start + tok) * p.qs + (int64_t)(h * G + g) * D + 8 * ln.hf;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) q[d] = *(const ta::u4 *)(qp + 16 * d);
+      });
   if (row < rows) {
     const float l = st.l + ta::other_half(st.l);
     const float inv = l > 0.f ? 1.f / l : l;  // (a NaN stays)
@@ -235,7 +160,7 @@ extern "C" gkv_status gkv_prompt_attn(const void *q, const void *k, const void *
   p.tiles[n] = (int32_t)tiles;
   if (tiles * Hkv > 0x7fffffff) return GKV_E_UNSUPPORTED;
   const dim3 grid((unsigned)(tiles * Hkv)), blk(64 * kWaves);
-  const size_t lds = 4 * kTileBytes;
+  const size_t lds = ta::kAttendLds;
   if (dtype == GKV_F16)
     hipLaunchKernelGGL((prompt_kernel<ta::F16, kWaves>), grid, blk, lds, (hipStream_t)stream, p);
   else

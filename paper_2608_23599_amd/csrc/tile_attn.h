@@ -30,6 +30,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#pragma clang diagnostic ignored "-Winline-asm"  // the LDS copies set M0 themselves (dma16)
+
 namespace gkv {
 namespace ta {
 
@@ -170,17 +172,32 @@ __device__ __forceinline__ uint32_t bad_halves(uint32_t x) {
   return ((x & lo) == lo ? 0xFFFFu : 0u) | ((x & (lo << 16)) == (lo << 16) ? 0xFFFF0000u : 0u);
 }
 
-// S^T of NT 32-token groups.
-template <class T, int NT>
-__device__ __forceinline__ void scores(f16v (&s)[NT], const Lane &ln, const u4 (&q)[8], uint32_t kbase) {
+// What the scores of a 64-token tile start from: 0, or the tile's 64 floats at `bias`, in the
+// accumulators' order.
+template <bool kBias>
+__device__ __forceinline__ void start_scores(f16v (&s)[2], const Lane &ln, uint32_t bias) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+    for (int i = 0; i < 4; ++i) {
+      u4 x = {0, 0, 0, 0};
+      if (kBias) x = lds_u4(bias + 128 * t + 32 * i + 16 * ln.hf);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t w = x[k];
+        s[t][4 * i + k] = __builtin_bit_cast(float, w);
+      }
+    }
+}
+
+// S^T of a 64-token tile.
+template <class T, bool kBias>
+__device__ __forceinline__ void scores(f16v (&s)[2], const Lane &ln, const u4 (&q)[8], uint32_t kbase, uint32_t bias) {
+  start_scores<kBias>(s, ln, bias);
 #pragma unroll
   for (int d = 0; d < 8; ++d)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[t] = T::mfma(lds_u4(kbase + (ln.k0 ^ (d << 5)) + t * 8192), q[d], s[t]);
+    for (int t = 0; t < 2; ++t) s[t] = T::mfma(lds_u4(kbase + (ln.k0 ^ (d << 5)) + t * 8192), q[d], s[t]);
 }
 
 // Scores of tokens whose bit in vis (of this lane's row) is clear become -infinity.
@@ -235,14 +252,6 @@ __device__ __forceinline__ void weights(u4 (&p)[2 * NT], Rows &r, const f16v (&s
 #pragma unroll
   for (int j = 0; j < 2 * NT; ++j) asm volatile("" : "+v"(p[j]));
   asm volatile("" : "+v"(r.l));
-}
-
-template <class T, int NT, bool kTr>
-__device__ __forceinline__ void outputs(Rows &r, const Lane &ln, const u4 (&p)[2 * NT], uint32_t vbase) {
-#pragma unroll
-  for (int kk = 0; kk < 2 * NT; ++kk)
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct) r.o[ct] = T::mfma(value_operand<kTr>(ln, vbase, kk, ct), p[kk], r.o[ct]);
 }
 
 // Values (token t, channels 32 ct + 8 j + 4 hf .. + 3) of a tile.
@@ -327,9 +336,9 @@ __device__ __forceinline__ void add_odd(Rows &r, const u4 &odd) {
 // The value product of one 64-token tile and the key product of the next, one MFMA after the
 // other with the operands read kAhead products before (the order is pinned: left alone, the
 // compiler reads one ahead and every product waits for LDS).
-template <class T, bool kTr>
+template <class T, bool kTr, bool kBias>
 __device__ __forceinline__ void multiply(Rows &r, f16v (&s)[2], const Lane &ln, const u4 (&p)[4], const u4 (&q)[8],
-                                         uint32_t vbase, uint32_t kbase) {
+                                         uint32_t vbase, uint32_t kbase, uint32_t bias) {
   constexpr int kAhead = 6;
   u4 x[kAhead];
   auto operand = [&](int i) {
@@ -338,10 +347,7 @@ __device__ __forceinline__ void multiply(Rows &r, f16v (&s)[2], const Lane &ln, 
   };
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) x[i] = operand(i);
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+  start_scores<kBias>(s, ln, bias);
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
     __builtin_amdgcn_sched_barrier(0);
@@ -351,6 +357,102 @@ __device__ __forceinline__ void multiply(Rows &r, f16v (&s)[2], const Lane &ln, 
     if (i + kAhead < 32) x[i % kAhead] = operand(i + kAhead);
   }
   __builtin_amdgcn_sched_barrier(0);
+}
+
+// ---------------------------------------------------------------- a workgroup's pass
+constexpr int kTile = 64;                  // tokens of a tile
+constexpr int kTileBytes = kTile * 128 * 2;  // of its keys, or of its values
+constexpr int kBiasBytes = kTile * 4;
+constexpr int kAttendLds = 4 * kTileBytes;   // two tiles; with biases 2 kBiasBytes more
+
+// LDS copies of 16 bytes a lane, lane after lane from a wave-uniform LDS address.
+__device__ __forceinline__ void dma16(uint32_t voff, const void *base, uint32_t lds) {
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(m0v) : "memory", "m0");
+}
+
+// The rows of a workgroup over tiles t0 .. t1 - 1 (t0 < t1), those before `full` seen whole by
+// every row; seen(t) gives a lane's row's visible tokens of any other.  src.keys(t, lds)
+// and src.values(t, lds) issue the wavefront's part of a tile's copies.  load() gets the queries, after the first
+// copies are on their way.
+//
+// The two wavefronts of a SIMD (w and w + WAVES / 2) work half a tile apart: while one
+// multiplies (the last tile's values, this tile's keys) the other forms weights.  In the same
+// phase they wait for one unit together: the MFMAs ran 43% of the time and the vector
+// instructions 49% (16k tokens x 28 heads: 1975 us; half a tile apart 1744).
+//
+// Intervals, each ended by a barrier: the first wavefronts' key product of tile t is in interval
+// 2 t, the second ones' in 2 t + 1.  Keys t + 1 and values t are copied from the start of
+// interval 2 t on (whose buffers were last read in 2 t - 1) and have arrived at the end of
+// 2 t + 1.
+template <class T, int WAVES, bool kTr, bool kBias, class Src, class Seen, class Load>
+__device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uint32_t lds, int wave, int t0, int t1,
+                                       int full, float sl2, const Src &src, const Seen &seen, const Load &load) {
+  const bool second = wave >= WAVES / 2;
+  auto keys = [&](int t) { return lds + (t & 1) * kTileBytes; };
+  auto values = [&](int t) { return lds + (2 + (t & 1)) * kTileBytes; };
+  auto bias = [&](int t) { return lds + 4 * kTileBytes + (t & 1) * kBiasBytes; };
+  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+  auto meet = [] {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto copy_keys = [&](int t) { src.keys(t, keys(t), bias(t)); };
+  auto copy = [&](int t) {
+    if (t + 1 < t1) copy_keys(t + 1);
+    if (t < t1) src.values(t, values(t));
+  };
+  auto before = [&](int t) {  // the value product of tile t
+    if (!second) arrived();
+    meet();
+    if (!second) copy(t + 1);
+  };
+  auto after = [&](int t) {
+    if (second) arrived();
+    meet();
+    if (second) copy(t + 2);
+  };
+  copy_keys(t0);
+  load();
+  // the queries have arrived (the loop's copies are in flight when they are used: a wait for
+  // their loads there would wait for the copies)
+#pragma unroll
+  for (int d = 0; d < 8; ++d) asm volatile("" : "+v"(q[d]));
+  st.init();
+  f16v s[2];
+  u4 pr[4];
+  if (full > t1 - 1) full = t1 - 1;
+  arrived();
+  meet();
+  copy(t0);
+  if (second) {
+    arrived();
+    meet();
+  }
+  scores<T, kBias>(s, ln, q, keys(t0), bias(t0));
+  after(t0 - 1);
+  int t = t0;
+  for (; t < full; ++t) {
+    weights<T, 2>(pr, st, s, sl2);
+    before(t);
+    multiply<T, kTr, kBias>(st, s, ln, pr, q, values(t), keys(t + 1), bias(t + 1));
+    after(t);
+  }
+  u4 odd = {0, 0, 0, 0};  // infinities and NaN among the values from here on
+  for (;; ++t) {
+    const uint64_t vis = seen(t);
+    mask_scores<2>(s, ln, vis);
+    weights<T, 2>(pr, st, s, sl2);
+    before(t);
+    const bool clean = find_odd<T, 2, kTr>(ln, values(t), vis, odd);
+    outputs_clean<T, 2, kTr>(st, ln, pr, values(t), clean);
+    if (t == t1 - 1) break;
+    scores<T, kBias>(s, ln, q, keys(t + 1), bias(t + 1));
+    after(t);
+  }
+  if (!second) meet();
+  add_odd(st, odd);
 }
 
 }  // namespace ta
