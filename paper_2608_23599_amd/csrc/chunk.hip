@@ -27,8 +27,7 @@ using ta::u4;
 using T16 = ta::F16;
 
 constexpr int kMaxSeqs = GKV_MAX_CHUNK_SEQS;
-constexpr int kRecTile = P * D * 2;  // bytes of a tile's keys, or of its values
-constexpr int kPart = D + 2;         // floats of a row's partial: O, m, l
+constexpr int kPart = D + 2;  // floats of a row's partial: O, m, l
 
 struct ChunkParams {
   const uint16_t *q;
@@ -56,9 +55,8 @@ struct ChunkParams {
 
 // ---------------------------------------------------------------- records to tiles
 // Table entries are the same for a whole wavefront and no kernel here writes them: scalar loads,
-// which wait apart from the records' vector loads (as vector loads they stood in line with
-// those, and every block waited for its table entries alone: 241 us against XXX for 2 tokens
-// over 8 x 128k).
+// which wait apart from the records' vector loads (as vector loads they would stand in line with
+// those, and every block would wait for its table entries alone).
 typedef const __attribute__((address_space(4))) uint64_t *ScalarU64;
 typedef const __attribute__((address_space(4))) uint32_t *ScalarU32;
 __device__ __forceinline__ uint64_t table64(const void *t, int64_t i) { return ((ScalarU64)(uintptr_t)t)[i]; }
@@ -241,6 +239,30 @@ __device__ __forceinline__ void key_words_any(uint32_t (&y)[16], const Raw &x, i
   else key_words<GKV_EXACT>(y, x, head, kg);
 }
 
+// A lane's value chunk of a centroid block: its channels' centroids, four to a channel, by the two
+// bits of each of its four tokens.
+__device__ __forceinline__ void centroid_words(uint32_t (&y)[16], const u4 (&cent)[4], uint32_t ids) {
+  uint32_t sel[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t a = ids >> (4 * i) & 3u, b = ids >> (4 * i + 2) & 3u;
+    sel[i] = (2 * a) | (2 * a + 1) << 8 | (2 * b) << 16 | (2 * b + 1) << 24;
+  }
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int c = q >> 1;
+    y[q] = __builtin_amdgcn_perm(cent[c >> 1][2 * (c & 1) + 1], cent[c >> 1][2 * (c & 1)], sel[q & 1]);
+  }
+}
+// Zeros for the tokens of page pg in drop.
+__device__ __forceinline__ void drop_words(uint32_t (&y)[16], uint64_t drop, int pg, int kg) {
+  const uint32_t d = (uint32_t)(drop >> (16 * pg)) >> (4 * kg);
+  const uint32_t keep[2] = {(d & 1 ? 0 : 0xFFFFu) | (d & 2 ? 0 : 0xFFFF0000u),
+                            (d & 4 ? 0 : 0xFFFFu) | (d & 8 ? 0 : 0xFFFF0000u)};
+#pragma unroll
+  for (int q = 0; q < 16; ++q) y[q] &= keep[q & 1];
+}
+
 // A lane's value chunk of page pg as fp16 pairs: words 2 c and 2 c + 1 are tokens 4 kg .. + 3 of
 // channel 16 c + m.  drop: the block's tokens that are not read, whose values become zero
 // (their weight is zero, but 0 * infinity is NaN).
@@ -251,18 +273,7 @@ __device__ __forceinline__ void value_words(uint32_t (&y)[16], const Raw &x, con
   if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
     stage_value_codes<LEVEL>(y, x, head, pg, lane, vtok);
   } else if constexpr (LEVEL == GKV_CENTROID) {
-    const uint32_t ids = table32(rec + KC * D * 2, pg) >> (8 * kg);  // of the lane's four tokens
-    uint32_t sel[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t a = ids >> (4 * i) & 3u, b = ids >> (4 * i + 2) & 3u;
-      sel[i] = (2 * a) | (2 * a + 1) << 8 | (2 * b) << 16 | (2 * b + 1) << 24;
-    }
-#pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      const int c = q >> 1;
-      y[q] = __builtin_amdgcn_perm(x.w[c >> 1][2 * (c & 1) + 1], x.w[c >> 1][2 * (c & 1)], sel[q & 1]);
-    }
+    centroid_words(y, x.w, table32(rec + KC * D * 2, pg) >> (8 * kg));
   } else if constexpr (LEVEL == GKV_MEAN) {
 #pragma unroll
     for (int q = 0; q < 16; ++q) y[q] = x.w[q >> 3][(q >> 1) & 3];
@@ -270,13 +281,7 @@ __device__ __forceinline__ void value_words(uint32_t (&y)[16], const Raw &x, con
 #pragma unroll
     for (int q = 0; q < 16; ++q) y[q] = x.w[q >> 2][q & 3];
   }
-  if (drop) {
-    const uint32_t d = (uint32_t)(drop >> (16 * pg)) >> (4 * kg);
-    const uint32_t keep[2] = {(d & 1 ? 0 : 0xFFFFu) | (d & 2 ? 0 : 0xFFFF0000u),
-                              (d & 4 ? 0 : 0xFFFFu) | (d & 8 ? 0 : 0xFFFF0000u)};
-#pragma unroll
-    for (int q = 0; q < 16; ++q) y[q] &= keep[q & 1];
-  }
+  if (drop) drop_words(y, drop, pg, kg);
 }
 
 // The same of any level.
@@ -599,14 +604,25 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams 
 }
 
 // ---------------------------------------------------------------- few rows
-// At most 16 CT rows of a (sequence, KV head): every wavefront holds all of them and reads whole
-// blocks of its own, straight from the records into operands.  The records are laid out for
-// 16x16x32 MFMA (a lane's key chunk is the four operands of its page, its value chunk of two
-// pages the eight operands of 32 tokens), so nothing passes through LDS but the integer
-// levels' scales.  Scores are formed for 64 tokens, in the layout (lane l: row l & 15, token
-// 16 page + 4 (l >> 4) + i) that is the second product's operand layout again.  Bound by the
-// records' bytes and, near it, by the vector instructions that decode them (3.5 a pair).
+// At most 16 CT rows of a (sequence, KV head): every wavefront holds all of them and reads blocks of
+// its own.  The records are laid out for 16x16x32 MFMA (a lane's key chunk is the four
+// operands of its page, its value chunk of two pages the eight operands of 32 tokens), and
+// the scores' layout (lane l: row l & 15, token 16 page + 4 (l >> 4) + i) is the second
+// product's operand layout again.
+//
+// A record is copied to LDS as it is (asynchronous copies, 16 bytes a lane, with an exact or int8
+// chunk's pieces one behind the other so that a read finds each bank once) and decoded from
+// there: the copies hold no registers, so that two wavefronts fit a SIMD and a record is
+// always on its way.  A step is a block, or half an exact one; its values are copied from
+// the start of its key product on, the next step's keys from the end of that.  No other
+// vector memory instruction runs in the loop, so the wait for a record is a constant count.
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) f4 *LdsF4;
+typedef __attribute__((address_space(3))) f2 *LdsF2;
+
+constexpr int kFewWaves = 4;
+constexpr int kFewBuf = kSZBytes + P * D;  // an int8 record, the largest that is copied at once
 
 template <int CT>
 struct FewRows {
@@ -624,17 +640,16 @@ __device__ __forceinline__ float over_groups(float x) {  // the maximum over a r
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
-// Scores to packed probabilities (two dwords a page), raising the maxima as tile_attn.h does.
-template <int CT, int NP>
-__device__ __forceinline__ void few_weights(uint32_t (&p)[CT][2 * NP], FewRows<CT> &r, const f4 (&s)[NP][CT],
-                                            float sl2) {
+// Scores to packed probabilities (two words a page), raising the maxima as tile_attn.h does.
+template <int CT>
+__device__ __forceinline__ void few_weights(uint32_t (&p)[CT][8], FewRows<CT> &r, const f4 (&s)[4][CT], float sl2) {
   float top[CT];
   bool go = false;
 #pragma unroll
   for (int t = 0; t < CT; ++t) {
     top[t] = -__builtin_inff();
 #pragma unroll
-    for (int g = 0; g < NP; ++g)
+    for (int g = 0; g < 4; ++g)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], __builtin_fmaf(s[g][t][i], sl2, -r.m[t]));
     go |= top[t] > r.raise[t];
@@ -658,7 +673,7 @@ __device__ __forceinline__ void few_weights(uint32_t (&p)[CT][2 * NP], FewRows<C
 #pragma unroll
   for (int t = 0; t < CT; ++t)
 #pragma unroll
-    for (int g = 0; g < NP; ++g)
+    for (int g = 0; g < 4; ++g)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][t][2 * i], sl2, -r.m[t]));
@@ -669,255 +684,263 @@ __device__ __forceinline__ void few_weights(uint32_t (&p)[CT][2 * NP], FewRows<C
       }
 }
 
-// Scores of page g (keys as 16 words a lane).
-template <int CT>
-__device__ __forceinline__ void few_scores(f4 (&s)[CT], const uint32_t (&y)[16], const u4 (&q)[4][CT]) {
+// Copies of a record (exact: of its pages 2 half, 2 half + 1) to LDS, and how many they are.
+__device__ __forceinline__ void few_copy(const uint8_t *rec, int level, int half, uint32_t buf, int lane) {
+  if (level == GKV_EXACT) {
+    const uint8_t *src = rec + half * (kExactBytes / 2);
 #pragma unroll
-  for (int t = 0; t < CT; ++t) s[t] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 8; ++i) ta::dma16(lane * 64, src + (i >> 2) * 4096 + (i & 3) * 16, buf + i * 1024);
+    return;
+  }
+  if (level == GKV_MEAN) {
+    if (lane < kMeanBytes / 16) ta::dma16(lane * 16, rec, buf);
+    return;
+  }
+  if (level == GKV_CENTROID) {
+    ta::dma16(lane * 16, rec, buf);
+    if (lane < 1) ta::dma16(0, rec + 1024, buf + 1024);
+    return;
+  }
+  if (lane < kSZBytes / 16) ta::dma16(lane * 16, rec, buf);
+  rec += kSZBytes;
+  buf += kSZBytes;
+  if (level == GKV_INT8) {
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int t = 0; t < CT; ++t)
-      s[t] = mfma16(u4{y[4 * d], y[4 * d + 1], y[4 * d + 2], y[4 * d + 3]}, q[d][t], s[t]);
-}
-template <int CT>
-__device__ __forceinline__ void few_mask(f4 (&s)[4][CT], const uint64_t (&vis)[CT], int kg) {
-#pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    const uint64_t w = vis[t] >> (4 * kg);
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[g][t][i] = w >> (16 * g + i) & 1 ? s[g][t][i] : -__builtin_inff();
+    for (int i = 0; i < 8; ++i) ta::dma16(lane * 32, rec + (i >> 1) * 2048 + (i & 1) * 16, buf + i * 1024);
+  } else {
+    for (int i = 0; i < level; ++i) ta::dma16(lane * 16, rec + i * 1024, buf + i * 1024);
   }
 }
-// The value product of pages 2 pp and 2 pp + 1.
-template <int CT>
-__device__ __forceinline__ void few_outputs(FewRows<CT> &r, const uint32_t (&y)[2][16], const uint32_t (&w)[CT][8],
-                                            int pp) {
-#pragma unroll
-  for (int c = 0; c < 8; ++c)
-#pragma unroll
-    for (int t = 0; t < CT; ++t)
-      r.o[c][t] = mfma16(u4{y[0][2 * c], y[0][2 * c + 1], y[1][2 * c], y[1][2 * c + 1]},
-                         u4{w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]}, r.o[c][t]);
+// Waits until at most the copies of a record of this level (none: -1) are on their way.
+__device__ __forceinline__ void few_wait(int level) {
+  if (level == GKV_INT4) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+  else if (level == GKV_INT2) asm volatile("s_waitcnt vmcnt(3)" ::: "memory");
+  else if (level == GKV_INT8) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+  else if (level == GKV_EXACT) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  else if (level == GKV_CENTROID) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+  else if (level == GKV_MEAN) asm volatile("s_waitcnt vmcnt(1)" ::: "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
+// LDS reads of the buffer that is copied over next have returned.
+__device__ __forceinline__ void few_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// The first 64 bytes a lane needs of a record's codes or rows, as four 16-byte loads whose
-// addresses alone go by the level (int4: all four pages; int8: two; int2: four, half of each
-// load another lane's; exact: one; one-centroid keys: the row): so they can be in flight
-// across the branches that the levels take.
-__device__ __forceinline__ void load_ahead(u4 (&y)[4], const uint8_t *rec, int level, int lane) {
-  const uint8_t *at = rec + (level == GKV_EXACT ? lane * 64
-                             : level == GKV_INT8 ? kSZBytes + lane * 32
-                             : level == GKV_INT4 ? kSZBytes + lane * 16
-                             : level == GKV_INT2 ? kSZBytes + (lane & ~1) * 8
-                                                 : (lane >> 4) * 16);
-  const int s1 = level == GKV_INT4 ? 1024 : level == GKV_INT2 ? 512 : level == GKV_MEAN || level == GKV_CENTROID ? 64 : 16;
-  const int s2 = level == GKV_INT8 ? 2048 : 2 * s1;
-  y[0] = *(const u4 *)at;
-  y[1] = *(const u4 *)(at + s1);
-  y[2] = *(const u4 *)(at + s2);
-  y[3] = *(const u4 *)(at + s1 + s2);
-}
-// A lane's chunk of page g: from what was loaded ahead, or loaded now.
-template <int TENSOR, int LEVEL>
-__device__ __forceinline__ void take(Raw &x, const u4 (&y)[4], const uint8_t *rec, int g, int lane) {
-  if constexpr (LEVEL == GKV_INT4) {
-    x.w[0] = y[g];
-  } else if constexpr (LEVEL == GKV_INT2) {
-    x.w[0][0] = lane & 1 ? y[g][2] : y[g][0];
-    x.w[0][1] = lane & 1 ? y[g][3] : y[g][1];
-  } else if (LEVEL == GKV_INT8 && g < 2) {
-    x.w[0] = y[2 * g];
-    x.w[1] = y[2 * g + 1];
-  } else if ((LEVEL == GKV_EXACT && g == 0) || (LEVEL == GKV_MEAN && TENSOR == GKV_KEYS)) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.w[i] = y[i];
+// The codes of a lane's chunk of page g in a copied record.
+template <int BITS>
+__device__ __forceinline__ void few_codes(Raw &x, uint32_t buf, int g, int lane) {
+  const uint32_t at = buf + kSZBytes;
+  if constexpr (BITS == 8) {
+    x.w[0] = ta::lds_u4(at + 2 * g * 1024 + lane * 16);
+    x.w[1] = ta::lds_u4(at + (2 * g + 1) * 1024 + lane * 16);
+  } else if constexpr (BITS == 4) {
+    x.w[0] = ta::lds_u4(at + g * 1024 + lane * 16);
   } else {
-    load_raw<TENSOR>(x, rec, LEVEL, g, lane);
+    const u2 y = *(LdsW2)(uintptr_t)(at + g * 512 + lane * 8);
+    x.w[0][0] = y[0];
+    x.w[0][1] = y[1];
   }
 }
+__device__ __forceinline__ uint32_t lds_u16(uint32_t at) {
+  return *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)at;
+}
 
-// A block that every row sees whole, but for the tokens in x.drop: its scores ...
-template <int LEVEL, int CT>
-__device__ __forceinline__ void few_keys(f4 (&s)[4][CT], const Visit &x, const u4 (&ahead)[4], const u4 (&q)[4][CT],
-                                         float sl2, uint32_t head, int lane) {
-  const int kg = lane >> 4;
-  uint32_t y[16];
-  if constexpr (LEVEL == GKV_MEAN) {
-    // one key stands for all the block's tokens: its weight times their number, in the first
-    // group's first place alone
-    Raw k;
-    take<GKV_KEYS, LEVEL>(k, ahead, x.k, 0, lane);
-    key_words<LEVEL>(y, k, head, kg);
-    few_scores<CT>(s[0], y, q);
-    const int n = P - __popcll(x.drop);
-    const float more = __builtin_amdgcn_logf((float)n) / sl2, no = -__builtin_inff();
-#pragma unroll
-    for (int t = 0; t < CT; ++t)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[g][t][i] = g == 0 && i == 0 && kg == 0 && n ? s[0][t][0] + more : no;
+// A lane's key chunk of page g: words 4 j .. 4 j + 3 are channels 32 j + 8 kg .. + 7.
+template <int LEVEL>
+__device__ __forceinline__ void few_key_words(uint32_t (&y)[16], uint32_t buf, int g, int lane) {
+  const int kg = lane >> 4, m = lane & 15;
+  if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
+    Raw x;
+    few_codes<LEVEL>(x, buf, g, lane);
+    stage_key_codes<LEVEL>(y, x, buf, kg);
   } else {
-    Raw k[4];
+    uint32_t at = buf + g * 4096 + lane * 16, step = 1024;
+    if constexpr (LEVEL == GKV_CENTROID) {
+      const uint32_t ids = *(__attribute__((address_space(3))) const uint32_t *)(uintptr_t)(buf + KC * D * 2 + 4 * g);
+      at = buf + (ids >> (2 * m) & 3u) * (D * 2) + 16 * kg;
+      step = 64;
+    } else if constexpr (LEVEL == GKV_MEAN) {
+      at = buf + 16 * kg;
+      step = 64;
+    }
 #pragma unroll
-    for (int g = 0; g < 2; ++g) take<GKV_KEYS, LEVEL>(k[g], ahead, x.k, g, lane);
+    for (int j = 0; j < 4; ++j) {
+      const u4 a = ta::lds_u4(at + j * step);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      if (g + 2 < 4) take<GKV_KEYS, LEVEL>(k[g + 2], ahead, x.k, g + 2, lane);
-      key_words<LEVEL>(y, k[g], head, kg);
-      few_scores<CT>(s[g], y, q);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < 4; ++i) y[4 * j + i] = a[i];
     }
   }
 }
-// ... and, with their weights, its outputs.
-template <int LEVEL, int CT>
-__device__ __forceinline__ void few_values(FewRows<CT> &r, const uint32_t (&w)[CT][8], const Visit &x,
-                                           const u4 (&ahead)[4], bool vtok, uint32_t head, int lane) {
-  if constexpr (LEVEL == GKV_MEAN) {
-    Raw v;
-    load_raw<GKV_VALUES>(v, x.v, LEVEL, 0, lane);
+
+// What the values of a copied record are decoded with: scales and zeros (per channel: of the
+// lane's eight, channel 16 c + m in half c & 1 of word c >> 1), or a centroid block's rows.
+template <int LEVEL>
+struct FewValues {
+  u4 a[LEVEL == GKV_CENTROID ? 4 : 2];
+  __device__ __forceinline__ void init(uint32_t buf, int lane, bool vtok) {
+    const int m = lane & 15;
+    if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
+      if (!vtok)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {  // entry 32 (m >> 2) + 4 c + (m & 3) holds channel 16 c + m
+            const uint32_t at = buf + 256 * k + 2 * (32 * (m >> 2) + (m & 3)) + 16 * c;
+            a[k][c] = lds_u16(at) | lds_u16(at + 8) << 16;
+          }
+    } else if constexpr (LEVEL == GKV_CENTROID) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = ta::lds_u4(buf + m * 64 + 16 * i);
+    }
+  }
+  // words 2 c and 2 c + 1: tokens 4 kg .. + 3 of page g, channel 16 c + m
+  __device__ __forceinline__ void words(uint32_t (&y)[16], uint32_t buf, int g, int lane, bool vtok) const {
+    const int kg = lane >> 4;
+    if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
+      Raw x;
+      few_codes<LEVEL>(x, buf, g, lane);
+      if (vtok) {
+        const u2 s = *(LdsW2)(uintptr_t)(buf + (16 * g + 4 * kg) * 2);
+        const u2 z = *(LdsW2)(uintptr_t)(buf + 128 + (16 * g + 4 * kg) * 2);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) y[q] = decoded(code_pair<LEVEL>(x.w, q), s[q & 1], z[q & 1]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const int c = q >> 1;
+          y[q] = __builtin_bit_cast(uint32_t,
+                                    __builtin_elementwise_fma(code_pair<LEVEL>(x.w, q), twice(a[0][c >> 1], c & 1),
+                                                              twice(a[1][c >> 1], c & 1)));
+        }
+      }
+    } else if constexpr (LEVEL == GKV_CENTROID) {
+      const uint32_t ids =
+          *(__attribute__((address_space(3))) const uint32_t *)(uintptr_t)(buf + KC * D * 2 + 4 * g) >> (8 * kg);
+      centroid_words(y, a, ids);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u4 b = ta::lds_u4(buf + g * 4096 + j * 1024 + lane * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[4 * j + i] = b[i];
+      }
+    }
+  }
+};
+
+// The operands of two pages of a copied record: keys, four a page; values, one for each 16
+// channels.  Only these depend on the level, so that the products' accumulators stand in no
+// branch (in one for each level they were copied from one to the next: 1100 moves).
+template <int LEVEL>
+__device__ __forceinline__ void few_key_pair(u4 (&a)[8], uint32_t buf, int pp, int lane) {
+#pragma unroll
+  for (int g = 0; g < (LEVEL == GKV_MEAN ? 1 : 2); ++g) {
+    uint32_t y[16];
+    few_key_words<LEVEL>(y, buf, 2 * pp + g, lane);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) a[4 * g + d] = u4{y[4 * d], y[4 * d + 1], y[4 * d + 2], y[4 * d + 3]};
+  }
+}
+template <int LEVEL>
+__device__ __forceinline__ void few_value_pair(u4 (&a)[8], const Visit &x, int half, uint32_t buf, int pp, bool vtok,
+                                               int lane) {
+  if constexpr (LEVEL == GKV_MEAN) {  // the one key's place alone
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t v = lds_u16(buf + 2 * (16 * c + (lane & 15)));
+      a[c] = u4{lane < 16 ? v : 0, 0, 0, 0};
+    }
+  } else {
+    FewValues<LEVEL> v;
+    v.init(buf, lane, vtok);
+    uint32_t y[2][16];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      v.words(y[g], buf, 2 * pp + g, lane, vtok);
+      // a token that is read elsewhere has weight 0, but 0 * infinity is NaN (an integer
+      // block's infinities and NaN are those of whole channels)
+      if ((LEVEL == GKV_EXACT || LEVEL == GKV_CENTROID) && x.drop) drop_words(y[g], x.drop, 2 * (half + pp) + g, lane >> 4);
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) a[c] = u4{y[0][2 * c], y[0][2 * c + 1], y[1][2 * c], y[1][2 * c + 1]};
+  }
+}
+
+// Infinities and NaN among an exact half block's values where some row does not see all of it:
+// out of the product, and noted for the rows that see them (two bits an output, as in
+// ta::find_odd).  The copied values are made clean in place.
+template <int CT>
+__device__ __forceinline__ void few_odd(u4 (&odd)[CT], const uint64_t (&vis)[CT], uint32_t buf, int half, int lane) {
+  const int kg = lane >> 4;
+  float zero = 0.f;
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    const u4 a = ta::lds_u4(buf + i * 1024 + lane * 16);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) zero = T16::times0(a[k], zero);
+  }
+  if (__builtin_expect(!__any(zero != zero), 1)) return;
+  // token 16 g + 4 a + b, channel 16 c + 4 kg + i: lane 16 a + 4 kg + i's word 2 c + (b >> 1)
+#pragma unroll 1
+  for (int tok = 0; tok < 32; ++tok) {
+    const uint32_t at = buf + (tok >> 4) * 4096 + (16 * (tok >> 2 & 3) + 4 * kg) * 16 + 2 * (tok & 3);
 #pragma unroll
     for (int c = 0; c < 8; ++c)
 #pragma unroll
-      for (int t = 0; t < CT; ++t)
-        r.o[c][t] = mfma16(u4{v.w[c >> 2][c & 3] & 0xFFFFu, 0, 0, 0}, u4{w[t][0], 0, 0, 0}, r.o[c][t]);
-  } else {
-    Raw v[4];
-#pragma unroll
-    for (int g = 0; g < 2; ++g) take<GKV_VALUES, LEVEL>(v[g], ahead, x.v, g, lane);
-#pragma unroll
-    for (int pp = 0; pp < 2; ++pp) {
-      uint32_t y[2][16];
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        value_words<LEVEL>(y[g], v[2 * pp + g], x.v, x.drop, head, 2 * pp + g, lane, vtok);
-        if (!pp) take<GKV_VALUES, LEVEL>(v[2 + g], ahead, x.v, 2 + g, lane);
-      }
-      few_outputs<CT>(r, y, w, pp);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-}
-
-// A block that some row sees in part (the last ones of a sequence), of any level: its keys, then
-// its values pass through LDS (16 KB at buf), where infinities and NaN among the values
-// are found, kept out of the product and noted for the rows that see them (two bits an
-// output, as in find_odd).
-template <int CT>
-__device__ __forceinline__ void few_part(FewRows<CT> &r, const ChunkParams &p, const Visit &x, const u4 (&q)[4][CT],
-                                         const uint64_t (&vis)[CT], u4 (&odd)[CT], uint32_t head, uint32_t buf, int lane) {
-  const int kg = lane >> 4;
-  auto put = [&](const uint32_t (&y)[16], int g) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *(LdsW4)(uintptr_t)(buf + g * 4096 + i * 1024 + lane * 16) = u4{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]};
-  };
-  auto get = [&](uint32_t (&y)[16], int g) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u4 a = ta::lds_u4(buf + g * 4096 + i * 1024 + lane * 16);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) y[4 * i + k] = a[k];
-    }
-  };
-#pragma unroll 1
-  for (int g = 0; g < 4; ++g) {
-    Raw k;
-    uint32_t y[16];
-    load_raw<GKV_KEYS>(k, x.k, x.level, g, lane);
-    key_words_any(y, k, x.level, head, kg);
-    put(y, g);
-  }
-  f4 s[4][CT];
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    uint32_t y[16];
-    get(y, g);
-    few_scores<CT>(s[g], y, q);
-  }
-  few_mask<CT>(s, vis, kg);
-  uint32_t w[CT][8];
-  few_weights<CT, 4>(w, r, s, p.sl2);
-  float zero = 0.f;
-#pragma unroll 1
-  for (int g = 0; g < 4; ++g) {
-    Raw v;
-    uint32_t y[16];
-    load_raw<GKV_VALUES>(v, x.v, x.level, g, lane);
-    value_words_any(y, v, x, head, g, lane, p.vtok);
-    put(y, g);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) zero = T16::times0(y[i], zero);
-  }
-  if (__builtin_expect(__any(zero != zero), 0)) {
-    // output (c, i) of a lane is channel 16 c + 4 kg + i; token 4 a + b of a page lies in
-    // lane 16 a + 4 kg + i's words 2 c, 2 c + 1 at half b
-#pragma unroll 1
-    for (int tok = 0; tok < P; ++tok) {
-      const uint32_t at = buf + (tok >> 4) * 4096 + (16 * (tok >> 2 & 3) + 4 * kg) * 16 + 2 * (tok & 3);
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t h = *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)(
-              at + (c >> 1) * 1024 + (c & 1) * 8 + i * 16);
-          const uint32_t e = h & 0x7FFFu, b = e < T16::kInf ? 0u : e > T16::kInf ? 3u : h == e ? 1u : 2u;
-#pragma unroll
-          for (int t = 0; t < CT; ++t) odd[t][c >> 1] |= (vis[t] >> tok & 1 ? b : 0u) << (8 * (c & 1) + 2 * i);
-        }
-    }
-#pragma unroll 1
-    for (int g = 0; g < 4; ++g) {
-      uint32_t y[16];
-      get(y, g);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] &= ~ta::bad_halves<T16>(y[i]);
-      put(y, g);
-    }
-  }
-#pragma unroll
-  for (int pp = 0; pp < 2; ++pp)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u4 a = ta::lds_u4(buf + 2 * pp * 4096 + i * 1024 + lane * 16);
-      const u4 b = ta::lds_u4(buf + (2 * pp + 1) * 4096 + i * 1024 + lane * 16);
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t h = lds_u16(at + (c >> 1) * 1024 + (c & 1) * 8 + i * 16);
+        const uint32_t e = h & 0x7FFFu, b = e < T16::kInf ? 0u : e > T16::kInf ? 3u : h == e ? 1u : 2u;
 #pragma unroll
         for (int t = 0; t < CT; ++t)
-          r.o[2 * i + k][t] = mfma16(u4{a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1]},
-                                     u4{w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]},
-                                     r.o[2 * i + k][t]);
-    }
+          odd[t][c >> 1] |= (vis[t] >> (32 * half + tok) & 1 ? b : 0u) << (8 * (c & 1) + 2 * i);
+      }
+  }
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    u4 a = ta::lds_u4(buf + i * 1024 + lane * 16);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a[k] &= ~ta::bad_halves<T16>(a[k]);
+    *(LdsW4)(uintptr_t)(buf + i * 1024 + lane * 16) = a;
+  }
 }
 
-constexpr int kFewWaves = 4;
-constexpr int kFewRow = D + 4;             // floats of a row in the wavefronts' merge
+#define GKV_LEVELS(level, f, ...)                                \
+  do {                                                           \
+    if (level == GKV_INT4) f<GKV_INT4>(__VA_ARGS__);             \
+    else if (level == GKV_INT2) f<GKV_INT2>(__VA_ARGS__);        \
+    else if (level == GKV_INT8) f<GKV_INT8>(__VA_ARGS__);        \
+    else if (level == GKV_EXACT) f<GKV_EXACT>(__VA_ARGS__);      \
+    else if (level == GKV_CENTROID) f<GKV_CENTROID>(__VA_ARGS__); \
+    else f<GKV_MEAN>(__VA_ARGS__);                               \
+  } while (0)
 
 template <int CT>
-__global__ void __launch_bounds__(64 * kFewWaves, CT == 1 ? 2 : 1) few_kernel(const ChunkParams p) {
+__global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(const ChunkParams p) {
   constexpr int kR = 16 * CT;
-  // a wavefront's part: a header and a block's keys or values, then its state
-  constexpr int kFewLds = 1024 + kRecTile > kR * kFewRow * 4 ? 1024 + kRecTile : kR * kFewRow * 4;
-  __shared__ __align__(16) float sh[kFewWaves * kFewLds / 4];
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)sh;
+  // the queries' operands, then each wavefront's two buffers; in the end its state
+  constexpr int kQ = CT * 4096;
+  __shared__ __align__(16) uint8_t sh[kQ + kFewWaves * 2 * kFewBuf];
+  static_assert((8 * 4 + 2) * CT * 256 * 2 <= sizeof(sh), "two wavefronts' states");
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)sh;
   const Job j = job_of(p, kR);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int kg = lane >> 4, m = lane & 15;
-  int tok[CT], g[CT];
-  u4 q[4][CT];
+  auto token = [&](int t) { return min(16 * t + m, j.rows - 1) / p.G; };  // rows past the last are copies
+  const int nvis = j.nblk + (p.nres + P - 1) / P;
+  const int split = p.split[j.s];
+  // every workgroup takes blocks from the whole context in turn, so that each gets as many of
+  // each level (in runs of blocks the ones with the exact blocks took a third longer)
+  const int v1 = nvis, stride = split * kFewWaves;
+  const uint32_t kbuf = lds + kQ + wave * 2 * kFewBuf, vbuf = kbuf + kFewBuf;
+  int at = j.part * kFewWaves + wave, half = 0;
+  Visit x, next;
+  if (at < v1) {
+    x = visit_at(p, j.u, at, j.nblk);
+    few_copy(x.k, x.level, 0, kbuf, lane);
+  }
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    const int rc = min(16 * t + m, j.rows - 1);  // rows past the last are copies, not stored
-    tok[t] = rc / p.G;
-    g[t] = rc - tok[t] * p.G;
-    const uint16_t *qp = p.q + (j.row0 + tok[t]) * p.qs + (int64_t)(j.h * p.G + g[t]) * D + 8 * kg;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) q[d][t] = *(const u4 *)(qp + 32 * d);
+  for (int t = 0; t < CT; ++t) {  // a wavefront copies channels 32 wave .. + 31
+    const int rc = min(16 * t + m, j.rows - 1), tok = rc / p.G, g = rc - tok * p.G;
+    *(LdsW4)(uintptr_t)(lds + (t * 4 + wave) * 1024 + lane * 16) =
+        *(const u4 *)(p.q + (j.row0 + tok) * p.qs + (int64_t)(j.h * p.G + g) * D + 8 * kg + 32 * wave);
   }
   FewRows<CT> r;
   u4 odd[CT];
@@ -929,113 +952,159 @@ __global__ void __launch_bounds__(64 * kFewWaves, CT == 1 ? 2 : 1) few_kernel(co
     r.raise[t] = -__builtin_inff();
     odd[t] = u4{0, 0, 0, 0};
   }
-  const int nvis = j.nblk + (p.nres + P - 1) / P;
-  const int split = p.split[j.s];
-  const int v0 = (int)((int64_t)nvis * j.part / split), v1 = (int)((int64_t)nvis * (j.part + 1) / split);
-  const uint32_t head = lds + wave * kFewLds;
-  int v = v0 + wave;
-  Visit x;
-  u4 ka[4], va[4], hd = {0, 0, 0, 0};
-  auto ahead = [&] {
-    if (is_int_level(x.level)) hd = load_head(x, lane);
-    load_ahead(ka, x.k, x.level, lane);
-  };
-  if (v < v1) {
-    x = visit_at(p, j.u, v, j.nblk);
-    ahead();
-  }
-  while (v < v1) {
-    const Visit now = x;
-    const int at = v;
-    v += kFewWaves;
-    if (v < v1) x = visit_at(p, j.u, v, j.nblk);
-    if (is_int_level(now.level)) store_head(head, hd, lane, p.vtok);
-    if (!whole_at(p, j, at, j.pos0)) {
-      uint64_t vis[CT];
-#pragma unroll
-      for (int t = 0; t < CT; ++t) vis[t] = seen_by(p, j, at, now.drop, j.pos0 + tok[t]);
-      few_part<CT>(r, p, now, q, vis, odd, head, head + 1024, lane);
-      ahead();
-      continue;
-    }
-    load_ahead(va, now.v, now.level, lane);
+  __syncthreads();
+  while (at < v1) {
+    const bool again = x.level == GKV_EXACT && half == 0;  // the block's other half is next
+    const int after = again ? at : at + stride;
+    next = x;
+    if (!again && after < v1) next = visit_at(p, j.u, after, j.nblk);
+    const bool whole = whole_at(p, j, at, j.pos0);
+    few_copy(x.v, x.level, half, vbuf, lane);
+    few_wait(x.level);
+    const bool two = x.level != GKV_EXACT && x.level != GKV_MEAN;  // pairs of pages
     f4 s[4][CT];
-#define GKV_LEVELS(f, ...)                                             \
-  if (now.level == GKV_INT4) f<GKV_INT4, CT>(__VA_ARGS__);             \
-  else if (now.level == GKV_INT2) f<GKV_INT2, CT>(__VA_ARGS__);        \
-  else if (now.level == GKV_INT8) f<GKV_INT8, CT>(__VA_ARGS__);        \
-  else if (now.level == GKV_EXACT) f<GKV_EXACT, CT>(__VA_ARGS__);      \
-  else if (now.level == GKV_CENTROID) f<GKV_CENTROID, CT>(__VA_ARGS__); \
-  else f<GKV_MEAN, CT>(__VA_ARGS__)
-    GKV_LEVELS(few_keys, s, now, ka, q, p.sl2, head, lane);
-    ahead();
-    if (now.drop && now.level != GKV_MEAN) {
-      uint64_t vis[CT];
 #pragma unroll
-      for (int t = 0; t < CT; ++t) vis[t] = ~now.drop;
-      few_mask<CT>(s, vis, kg);
+    for (int pp = 0; pp < 2; ++pp) {
+      if (pp == 0 || two) {
+        u4 a[8];
+        GKV_LEVELS(x.level, few_key_pair, a, kbuf, pp, lane);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          s[2 * pp][t] = s[2 * pp + 1][t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const u4 q = ta::lds_u4(lds + (t * 4 + d) * 1024 + lane * 16);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) s[2 * pp + g][t] = mfma16(a[4 * g + d], q, s[2 * pp + g][t]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[2][t][i] = s[3][t][i] = -__builtin_inff();
+      }
+      asm volatile("" ::: "memory");
+    }
+    if (x.level == GKV_MEAN) {
+      // one key stands for all the block's tokens: its weight times their number, in the first
+      // group's first place alone
+      const int n = P - __popcll(x.drop);
+      const float more = __builtin_amdgcn_logf((float)n) / p.sl2, no = -__builtin_inff();
+#pragma unroll
+      for (int t = 0; t < CT; ++t) {
+        s[0][t][0] = lane < 16 && n ? s[0][t][0] + more : no;
+        s[0][t][1] = s[0][t][2] = s[0][t][3] = no;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[1][t][i] = no;
+      }
+    }
+    few_read();
+    if (after < v1) few_copy(next.k, next.level, again ? 1 : 0, kbuf, lane);
+    uint64_t vis[CT];
+    if (!whole || (x.drop && x.level != GKV_MEAN)) {
+#pragma unroll
+      for (int t = 0; t < CT; ++t) {
+        vis[t] = whole ? ~x.drop : seen_by(p, j, at, x.drop, j.pos0 + token(t));
+        const uint64_t w = vis[t] >> (32 * half + 4 * kg);
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[g][t][i] = w >> (16 * g + i) & 1 ? s[g][t][i] : -__builtin_inff();
+      }
     }
     uint32_t w[CT][8];
-    few_weights<CT, 4>(w, r, s, p.sl2);
-    GKV_LEVELS(few_values, r, w, now, va, p.vtok, head, lane);
-#undef GKV_LEVELS
+    few_weights<CT>(w, r, s, p.sl2);
+    few_wait(after < v1 ? next.level : -1);
+    if (!whole) few_odd<CT>(odd, vis, vbuf, half, lane);  // an exact block (the host sees to it)
+#pragma unroll
+    for (int pp = 0; pp < 2; ++pp)
+      if (pp == 0 || two) {
+        u4 a[8];
+        GKV_LEVELS(x.level, few_value_pair, a, x, half, vbuf, pp, p.vtok, lane);
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int t = 0; t < CT; ++t)
+            r.o[c][t] = mfma16(a[c], u4{w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]}, r.o[c][t]);
+      }
+    few_read();
+    x = next;
+    half = again;
+    at = after;
   }
-  // the wavefronts' states, joined in LDS
-  __syncthreads();
+  // the wavefronts' states, joined two and two in LDS, each value in the lane that holds its like
 #pragma unroll
   for (int t = 0; t < CT; ++t) {
-    float l = r.l[t];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    r.l[t] += __shfl_xor(r.l[t], 16);
+    r.l[t] += __shfl_xor(r.l[t], 32);
 #pragma unroll
     for (int i = 0; i < 32; ++i) {  // the values that stayed out of the products
       const uint32_t b = odd[t][i >> 3] >> (8 * (i >> 2 & 1) + 2 * (i & 3)) & 3u;
       r.o[i >> 2][t][i & 3] += b == 0 ? 0.f : b == 3 ? __builtin_nanf("") : b == 1 ? __builtin_inff() : -__builtin_inff();
     }
-    float *row = sh + wave * (kFewLds / 4) + (16 * t + m) * kFewRow;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) *(f4 *)(row + 16 * c + 4 * kg) = r.o[c][t];
-    if (kg == 0) {
-      row[D] = r.m[t];
-      row[D + 1] = l;
-    }
   }
-  __syncthreads();
-  for (int i = wave; i < min(kR, j.rows); i += kFewWaves) {  // a row a wavefront, two channels a lane
-    float top = -__builtin_inff();
 #pragma unroll
-    for (int k = 0; k < kFewWaves; ++k) {
-      const float *row = sh + k * (kFewLds / 4) + i * kFewRow;
-      if (row[D + 1] != 0.f) top = fmaxf(top, row[D]);
-    }
-    float a = 0.f, b = 0.f, l = 0.f;
+  for (int n = 2; n >= 1; n >>= 1) {
+    __syncthreads();
+    const uint32_t mine = lds + (wave & (n - 1)) * ((8 * 4 + 2) * CT * 256) + lane * 16;
+    if (wave >= n && wave < 2 * n)
 #pragma unroll
-    for (int k = 0; k < kFewWaves; ++k) {
-      const float *row = sh + k * (kFewLds / 4) + i * kFewRow;
-      if (row[D + 1] == 0.f) continue;
-      const float f = __builtin_amdgcn_exp2f(row[D] - top);
-      a += f * row[2 * lane];
-      b += f * row[2 * lane + 1];
-      l += f * row[D + 1];
-    }
+      for (int t = 0; t < CT; ++t) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) *(LdsF4)(uintptr_t)(mine + (t * 8 + c) * 1024) = r.o[c][t];
+        *(LdsF2)(uintptr_t)(mine - lane * 8 + CT * 8192 + t * 512) = f2{r.m[t], r.l[t]};
+      }
+    __syncthreads();
+    if (wave < n)
+#pragma unroll
+      for (int t = 0; t < CT; ++t) {
+        const f2 ml = *(LdsF2)(uintptr_t)(mine - lane * 8 + CT * 8192 + t * 512);
+        // a state that has seen nothing has no maximum
+        const float top = r.l[t] == 0.f ? ml[0] : ml[1] == 0.f ? r.m[t] : fmaxf(r.m[t], ml[0]);
+        const float a = r.l[t] == 0.f ? 0.f : __builtin_amdgcn_exp2f(r.m[t] - top);
+        const float b = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
+        r.m[t] = top;
+        r.l[t] = r.l[t] * a + ml[1] * b;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const f4 o = *(LdsF4)(uintptr_t)(mine + (t * 8 + c) * 1024);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r.o[c][t][i] = r.o[c][t][i] * a + o[i] * b;
+        }
+      }
+  }
+  if (wave) return;
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+    const int i = 16 * t + m;
+    if (i >= j.rows) continue;
     if (split == 1) {
-      const float inv = l > 0.f ? 1.f / l : l;
-      const int tk = i / p.G, gg = i - tk * p.G;
-      *(uint32_t *)(p.out + (j.row0 + tk) * p.os + (int64_t)(j.h * p.G + gg) * D + 2 * lane) =
-          T16::pack(a * inv, b * inv);
+      const float inv = r.l[t] > 0.f ? 1.f / r.l[t] : r.l[t];
+      const int tok = i / p.G, g = i - tok * p.G;
+      uint16_t *op = p.out + (j.row0 + tok) * p.os + (int64_t)(j.h * p.G + g) * D + 4 * kg;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        *(u2 *)(op + 16 * c) = u2{T16::pack(r.o[c][t][0] * inv, r.o[c][t][1] * inv),
+                                  T16::pack(r.o[c][t][2] * inv, r.o[c][t][3] * inv)};
     } else {
       float *part = p.part + (part_row(p, j, kR) + i) * kPart;
-      *(float2 *)(part + 2 * lane) = make_float2(a, b);
-      if (lane == 0) *(float2 *)(part + D) = make_float2(top == -__builtin_inff() ? 0.f : top, l);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        *(float2 *)(part + 16 * c + 4 * kg) = make_float2(r.o[c][t][0], r.o[c][t][1]);
+        *(float2 *)(part + 16 * c + 4 * kg + 2) = make_float2(r.o[c][t][2], r.o[c][t][3]);
+      }
+      if (kg == 0) *(float2 *)(part + D) = make_float2(r.m[t], r.l[t]);
     }
   }
 }
+#undef GKV_LEVELS
 
-// Joins the partials of a row: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.  A wavefront
-// per row, two channels a lane.
+// Joins the partials of a row: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.  Sixteen lanes a
+// row, eight channels a lane; bound by the partials' bytes.
 __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, int rows_tile) {
-  const int lane = threadIdx.x & 63, h = blockIdx.y;
-  int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 15, h = blockIdx.y;
+  int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
   int s = 0;
   for (; s < p.nseq; ++s) {  // the row's sequence
     const int rows = p.split[s] > 1 ? p.n[s] * p.G : 0;
@@ -1050,23 +1119,34 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, i
   const int64_t step = (int64_t)tiles * rows_tile * kPart;
   const int n = p.split[s];
   float m = -__builtin_inff();
-  for (int i = lane; i < n; i += 64) {
+  for (int i = lane; i < n; i += 16) {
     const float2 ml = *(const float2 *)(part + i * step + D);
     if (ml.y != 0.f) m = fmaxf(m, ml.x);  // (one that saw nothing has no maximum)
   }
 #pragma unroll
-  for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-  float a = 0.f, b = 0.f, l = 0.f;
-#pragma unroll 8
+  for (int k = 8; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+  float o[8], l = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) o[k] = 0.f;
+#pragma unroll 4
   for (int i = 0; i < n; ++i) {
-    const float2 ml = *(const float2 *)(part + i * step + D), o = *(const float2 *)(part + i * step + 2 * lane);
+    const float *x = part + i * step;
+    const float2 ml = *(const float2 *)(x + D);
+    float2 y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = *(const float2 *)(x + 8 * lane + 2 * k);
     const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-    a += f * o.x;
-    b += f * o.y;
     l += f * ml.y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      o[2 * k] += f * y[k].x;
+      o[2 * k + 1] += f * y[k].y;
+    }
   }
   const float inv = l > 0.f ? 1.f / l : l;
-  *(uint32_t *)(p.out + (p.row0[s] + tok) * p.os + (int64_t)(h * p.G + g) * D + 2 * lane) = T16::pack(a * inv, b * inv);
+  *(u4 *)(p.out + (p.row0[s] + tok) * p.os + (int64_t)(h * p.G + g) * D + 8 * lane) =
+      u4{T16::pack(o[0] * inv, o[1] * inv), T16::pack(o[2] * inv, o[3] * inv), T16::pack(o[4] * inv, o[5] * inv),
+         T16::pack(o[6] * inv, o[7] * inv)};
 }
 
 // ---------------------------------------------------------------- host
@@ -1085,28 +1165,52 @@ struct Part {
                                           // rows and list tiles over all KV heads
 };
 
+// Shares of the contexts: every row tile of a sequence is cut into ceil(blocks / per) workgroups,
+// with the least `per` for which all workgroups are resident at once (fill of them), or in two
+// or three rounds where the row tiles alone are more.  What a workgroup takes beside its blocks
+// counts as kAlone blocks, and as kShared where it leaves a partial: 256 rows' partial is
+// 133 KB to write and to read again, 13 us at a compute unit's part of the memory rate,
+// where a block takes 2 us.
 gkv_status plan_part(Part &t, const gkv_cache *c, int64_t fill) {
+  constexpr int64_t kAlone = 2, kShared = 8, kRounds = 3;
   ChunkParams &p = t.p;
   const int G = c->Hq / c->Hkv;
   auto tiles = [&](int i) { return ((int64_t)p.n[i] * G + t.rows_tile - 1) / t.rows_tile; };
-  int64_t total = 0, plain = 0;
+  auto blocks = [&](int i) { return (int64_t)list_tiles(p.T[i], c->nres); };
+  int64_t total = 0, plain = 0, longest = 0;
   t.wgs = t.merged = t.part_rows = t.tiles = 0;
   for (int i = 0; i < p.nseq; ++i) {
-    total += tiles(i) * list_tiles(p.T[i], c->nres) * c->Hkv;
+    total += tiles(i) * blocks(i) * c->Hkv;
     plain += tiles(i) * c->Hkv;
+    longest = std::max(longest, blocks(i));
   }
-  // as many workgroups as are resident at once; no split where the row tiles alone are
-  int64_t per = plain >= fill ? 0x7fffffff : (total + fill - 1) / fill;
-  if (per < kLeastVisits) per = kLeastVisits;
+  auto count = [&](int64_t per) {
+    int64_t n = 0;
+    for (int i = 0; i < p.nseq; ++i) n += (blocks(i) + per - 1) / per * tiles(i);
+    return n * c->Hkv;
+  };
+  int64_t best = longest, cost = (longest + kAlone) * ((plain + fill - 1) / fill);
+  for (int64_t r = 1; r <= kRounds && p.nseq; ++r) {
+    if (plain > r * fill) continue;
+    int64_t lo = std::max<int64_t>(kLeastVisits, (total + r * fill - 1) / (r * fill)), hi = std::max(longest, lo);
+    while (lo < hi) {  // the least that fits
+      const int64_t mid = (lo + hi) / 2;
+      if (count(mid) <= r * fill) hi = mid;
+      else lo = mid + 1;
+    }
+    if (r * (lo + kShared) < cost) {
+      best = lo;
+      cost = r * (lo + kShared);
+    }
+  }
   for (int i = 0; i < p.nseq; ++i) {
-    int64_t s = list_tiles(p.T[i], c->nres) / per;
-    s = s < 1 ? 1 : s > 0xffff ? 0xffff : s;
+    const int64_t s = std::min<int64_t>((blocks(i) + best - 1) / best, 0xffff);
     p.split[i] = (uint16_t)s;
     p.wg0[i] = (int32_t)t.wgs;
     p.list0[i] = (int32_t)t.tiles;
     if (s > 1) t.merged += (int64_t)p.n[i] * G;
     t.wgs += s * tiles(i);
-    t.tiles += (int64_t)list_tiles(p.T[i], c->nres) * c->Hkv;
+    t.tiles += blocks(i) * c->Hkv;
     if (t.wgs * c->Hkv > 0x7fffffff || t.tiles > 0x7fffffff) return GKV_E_UNSUPPORTED;
   }
   p.wg0[p.nseq] = (int32_t)t.wgs;
@@ -1130,7 +1234,10 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
     if (T < 0) return GKV_E_ARG;
     if (n > T) return GKV_E_SHAPE;
     if (T > 0x7fffff00 || n * G > 0x7fffff00 || rows + n > 0x7fffffff) return GKV_E_UNSUPPORTED;
-    const bool few = n * G <= kFewMost;
+    bool few = n * G <= kFewMost;  // and the blocks that some row sees in part are exact
+    for (int h = 0; h < c->Hkv && few; ++h)
+      for (int64_t i = (T - n) / P; i < (T + P - 1) / P; ++i)
+        few &= c->level_host[((int64_t)b * c->Hkv + h) * c->nblk_cap + i] == GKV_EXACT;
     ChunkParams &p = few ? pl.few.p : pl.many.p;
     const int i = p.nseq++;
     p.seq[i] = (uint8_t)b;
@@ -1142,7 +1249,7 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
   }
   pl.few.rows_tile = (int)((most + 15) / 16 * 16);
   pl.many.rows_tile = 256;
-  gkv_status st = plan_part(pl.few, c, pl.few.rows_tile <= 16 ? 2 * kCus : kCus);
+  gkv_status st = plan_part(pl.few, c, pl.few.rows_tile <= 32 ? 2 * kCus : kCus);
   if (!st) st = plan_part(pl.many, c, kCus);
   if (st) return st;
   auto align = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
@@ -1229,7 +1336,7 @@ extern "C" gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const 
     }
     if (hipGetLastError() != hipSuccess) return GKV_E_HIP;
     if (t->merged) {
-      hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)((t->merged + 3) / 4), c->Hkv), dim3(256), 0, s, p,
+      hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)((t->merged + 15) / 16), c->Hkv), dim3(256), 0, s, p,
                          t->rows_tile);
       if (hipGetLastError() != hipSuccess) return GKV_E_HIP;
     }
