@@ -9,6 +9,7 @@ The function names mirror the C calls (``quantize_block``, ``demote``,
 ``append``); ``GradedCache`` owns the device tables and the slab arena of one
 layer's cache and marshals them into the ``gkv_cache`` descriptor.
 """
+import contextlib
 import ctypes
 import os
 
@@ -151,6 +152,14 @@ def _stream():
     return _raw_stream(torch.cuda.current_device())
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _on(device):
+    """Makes a device the current one for a call (nothing where it is)."""
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
 def block_bytes(level):
     return int(_block_bytes(level))
 
@@ -211,52 +220,80 @@ def allocate_levels(k, mass, qn, c, tau, window, rounding="up"):
     return lv
 
 
-def _rows_dev(x, what, device=None):
+def _rows_dev(x, what, heads=None, device=None):
     """Token rows [n][heads][128] on the device: fp16 or bf16, or fp16 bit patterns.  A view
     whose heads lie side by side in 16-byte aligned rows is taken as it is, any other one is
-    copied."""
+    copied.  Returns the tensor, n, heads and the elements from a token's rows to the next's."""
     if isinstance(x, np.ndarray):
         x = torch.from_numpy(np.ascontiguousarray(x).view(np.int16))
     if x.dtype == torch.int16:
         x = x.view(torch.float16)
-    if x.dtype not in (torch.float16, torch.bfloat16) or x.dim() != 3 or x.shape[2] != D:
+    if x.dtype not in (torch.float16, torch.bfloat16) or x.dim() != 3:
+        raise GkvError(-2, what)
+    n, h, d = x.shape
+    if d != D or heads is not None and h != heads:
         raise GkvError(-2, what)
     if device is not None and x.device != device or not x.is_cuda:
         x = x.to(device if device is not None else "cuda")
-    if x.shape[0] and (x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != D) or x.data_ptr() % 16 or
-                       (x.shape[0] > 1 and (x.stride(0) % 8 or x.stride(0) < x.shape[1] * D))):
+    if n == 0:
+        return x, n, h, h * D
+    st, sh, se = x.stride()
+    if n == 1:  # (a single row's stride is of no matter)
+        st = h * D
+    if se != 1 or h > 1 and sh != D or st % 8 or st < h * D or x.data_ptr() % 16:
         x = x.contiguous()
         if x.data_ptr() % 16:  # a contiguous view that starts inside a 16-byte unit
             x = x.clone()
-    return x
+        st = h * D
+    return x, n, h, st
 
 
-def _row_stride(x):
-    """Elements from one token's rows to the next one's."""
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * D
+def _rows_out(out, n, h, dtype, device, what):
+    """The rows a call writes, new or the caller's, and the elements between two tokens' rows."""
+    if out is None:
+        return torch.empty((n, h, D), dtype=dtype, device=device), h * D
+    if out.shape != (n, h, D) or out.dtype != dtype or out.device != device:
+        raise GkvError(-2, what)
+    if n and (out.stride(2) != 1 or h > 1 and out.stride(1) != D):
+        raise GkvError(-2, what)
+    return out, out.stride(0) if n > 1 else h * D
+
+
+def _int_list(lens, n, what, bits):
+    """lens as a list of n plain ints that `bits` bits hold (an int: the same n times)."""
+    if type(lens) is not list or any(type(x) is not int for x in lens):
+        a = np.asarray(lens)
+        if a.dtype.kind not in "iu" and a.size:
+            raise GkvError(-2, what)
+        if a.ndim == 0 and n is not None:
+            a = np.full(n, a)
+        if a.ndim != 1:
+            raise GkvError(-2, what)
+        lens = a.tolist()
+    if n is not None and len(lens) != n:
+        raise GkvError(-2, what)
+    if lens and (max(lens) >= 1 << bits - 1 or min(lens) < -(1 << bits - 1)):
+        raise GkvError(-2, what)
+    return lens
 
 
 def prompt_attn(q, k, v, lens, out=None):
     """gkv_prompt_attn: causal attention over packed prompts of lens tokens.  q [n][Hq][128],
     k, v [n][Hkv][128] (n = sum of lens), all fp16 (or its bits) or all bf16; views with a
     token stride are read in place.  Returns out [n][Hq][128] in the inputs' type."""
-    q = _rows_dev(q, "prompt_attn")
-    k, v = _rows_dev(k, "prompt_attn", q.device), _rows_dev(v, "prompt_attn", q.device)
-    lens = np.ascontiguousarray(lens, dtype=np.int64).reshape(-1)
-    n, Hq, _ = q.shape
-    if k.shape != v.shape or k.shape[0] != n or int(lens.sum()) != n:
+    q, n, Hq, qs = _rows_dev(q, "prompt_attn")
+    dev = q.device
+    k, nk, Hkv, ks = _rows_dev(k, "prompt_attn", None, dev)
+    v, nv, _, vs = _rows_dev(v, "prompt_attn", Hkv, dev)
+    lens = _int_list(lens, None, "prompt_attn", 64)
+    if nk != n or nv != n or sum(lens) != n:
         raise GkvError(-2, "prompt_attn")
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise GkvError(-1, "prompt_attn")
-    if out is None:
-        out = torch.empty((n, Hq, D), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or (
-            n and (out.stride(2) != 1 or out.stride(1) != D)):
-        raise GkvError(-2, "prompt_attn")
-    with torch.cuda.device(q.device):
-        _check(_prompt_attn(_dptr(q), _dptr(k), _dptr(v), _dptr(out), int(q.dtype == torch.bfloat16), k.shape[1], Hq,
-                            len(lens), _np_ptr(lens), _row_stride(q), _row_stride(k), _row_stride(v),
-                            _row_stride(out), _stream()), "prompt_attn")
+    out, os = _rows_out(out, n, Hq, q.dtype, dev, "prompt_attn")
+    with _on(dev):
+        _check(_prompt_attn(_dptr(q), _dptr(k), _dptr(v), _dptr(out), int(q.dtype == torch.bfloat16), Hkv, Hq,
+                            len(lens), (_i64 * len(lens))(*lens), qs, ks, vs, os, _stream()), "prompt_attn")
     return out
 
 
@@ -631,80 +668,69 @@ class GradedCache:
         self.demote([tuple(x) for x in J], to[:n])
         return [(int(b), int(h), int(i), o, int(t)) for (b, h, i), o, t in zip(J, olds, to[:n])]
 
-    def _counts(self, lens, what, dtype):
-        """One number per sequence as a contiguous array (an int: the same for all)."""
-        a = np.asarray(lens)
-        if a.ndim == 0:
-            a = np.full(self.B, a)
-        if a.shape != (self.B,) or a.dtype.kind not in "iu":
-            raise GkvError(-2, what)
-        if a.size and (int(a.max()) > np.iinfo(dtype).max or int(a.min()) < np.iinfo(dtype).min):
-            raise GkvError(-2, what)
-        return np.ascontiguousarray(a, dtype=dtype)
-
     def append_chunk(self, k_new, v_new, lens, profile=None):
         """gkv_append_chunk: append lens[b] tokens to every sequence (k_new, v_new packed fp16
         rows [n][Hkv][128], n = sum of lens; views with a token stride are read in place);
         then, with a ladder profile, demote what it lowers.  Returns the demotions
         [(b, h, blk, old, new)]."""
-        kd, vd = _rows_dev(k_new, "append_chunk", self._dev), _rows_dev(v_new, "append_chunk", self._dev)
-        lens = self._counts(lens, "append_chunk", np.int32)
+        kd, n, _, ks = _rows_dev(k_new, "append_chunk", self.Hkv, self._dev)
+        vd, nv, _, vs = _rows_dev(v_new, "append_chunk", self.Hkv, self._dev)
+        lens = _int_list(lens, self.B, "append_chunk", 32)
         if kd.dtype != torch.float16 or vd.dtype != torch.float16:
             raise GkvError(-1, "append_chunk")
-        if kd.shape != vd.shape or kd.shape[1] != self.Hkv or kd.shape[0] != int(lens.sum(dtype=np.int64)):
+        if nv != n or sum(lens) != n:
             raise GkvError(-2, "append_chunk")
-        have = self.lengths()
-        first = -(-np.maximum(have, 0) // P)
-        last = np.where(lens > 0, -(-(have + lens) // P), first)
-        opened = (last - first).tolist()
-        n = sum(opened) * self.Hkv
-        # K and V slots of one block side by side, sequence by sequence
-        kv = self.pool.alloc_many(EXACT, 2 * n) if n > 0 else np.empty(0, np.int64)
-        nk, nv = kv[0::2].copy(), kv[1::2].copy()
-        st = _append_chunk(ctypes.byref(self.c), _dptr(kd), _dptr(vd), _row_stride(kd), _row_stride(vd),
-                           _np_ptr(lens), _np_ptr(nk), _np_ptr(nv), n, _stream())
+        have = [self.T] * self.B if self.seq_len_host is None else self.seq_len_host.tolist()
+        # the blocks that open, (sequence, first, last): K and V slots of one block side by side
+        opens = [(b, -(-h // P), -(-(h + m) // P)) for b, (h, m) in enumerate(zip(have, lens))
+                 if m > 0 and h >= 0 and (h + m - 1) // P > (h - 1) // P]
+        slots = sum(hi - lo for _, lo, hi in opens) * self.Hkv
+        kv = nk = nv = None
+        if slots:
+            kv = self.pool.alloc_many(EXACT, 2 * slots)
+            nk, nv = kv[0::2].copy(), kv[1::2].copy()
+        with _on(self._dev):
+            st = _append_chunk(ctypes.byref(self.c), _dptr(kd), _dptr(vd), ks, vs, (_i32 * self.B)(*lens),
+                               _np_ptr(nk) if slots else None, _np_ptr(nv) if slots else None, slots, _stream())
         if st != 0:
-            for off in kv[::-1]:
-                self.pool.free(EXACT, int(off))
+            if slots:
+                for off in kv[::-1]:
+                    self.pool.free(EXACT, int(off))
             raise GkvError(st, "append_chunk")
         i = 0
-        for b, m in enumerate(opened):  # the mirrors follow the library only once the call succeeded
-            if m > 0:
-                at = (b, slice(None), slice(int(first[b]), int(last[b])))
-                self.koff_host[at] = nk[i:i + m * self.Hkv].reshape(self.Hkv, m)
-                self.voff_host[at] = nv[i:i + m * self.Hkv].reshape(self.Hkv, m)
-                i += m * self.Hkv
+        for b, lo, hi in opens:  # the mirrors follow the library only once the call succeeded
+            m = (hi - lo) * self.Hkv
+            self.koff_host[b, :, lo:hi] = nk[i:i + m].reshape(self.Hkv, hi - lo)
+            self.voff_host[b, :, lo:hi] = nv[i:i + m].reshape(self.Hkv, hi - lo)
+            i += m
         return self._cross(profile) if profile is not None else []
 
     def truncate(self, lens):
         """gkv_truncate: every sequence keeps its first lens[b] tokens (-1 for a retired one)."""
-        lens = self._counts(lens, "truncate", np.int64)
-        _check(_truncate(ctypes.byref(self.c), self.pool.h, _np_ptr(self.koff_host), _np_ptr(self.voff_host),
-                         _np_ptr(lens), _stream()), "truncate")
+        lens = _int_list(lens, self.B, "truncate", 64)
+        with _on(self._dev):
+            _check(_truncate(ctypes.byref(self.c), self.pool.h, self.koff_host.ctypes.data,
+                             self.voff_host.ctypes.data, (_i64 * self.B)(*lens), _stream()), "truncate")
 
     def chunk_attn(self, q, lens, out=None, ws=None):
         """gkv_chunk_attn: attention of the lens[b] newest tokens of every sequence over the
         cache they were appended to (q packed fp16 rows [n][Hq][128], n = sum of lens).
         Returns out [n][Hq][128] fp16."""
-        q = _rows_dev(q, "chunk_attn", self._dev)
-        lens = self._counts(lens, "chunk_attn", np.int32)
+        q, n, _, qs = _rows_dev(q, "chunk_attn", self.Hq, self._dev)
+        lens = _int_list(lens, self.B, "chunk_attn", 32)
         if q.dtype != torch.float16:
             raise GkvError(-1, "chunk_attn")
-        n = int(lens.sum(dtype=np.int64))
-        if q.shape[0] != n or q.shape[1] != self.Hq:
+        if sum(lens) != n:
             raise GkvError(-2, "chunk_attn")
-        if out is None:
-            out = torch.empty((n, self.Hq, D), dtype=torch.float16, device=self._dev)
-        elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or (
-                n and (out.stride(2) != 1 or out.stride(1) != D)):
-            raise GkvError(-2, "chunk_attn")
+        out, os = _rows_out(out, n, self.Hq, torch.float16, self._dev, "chunk_attn")
+        arr = (_i32 * self.B)(*lens)
         if ws is None:
             # of this call alone: its size goes by the lengths, and a captured graph keeps its own
-            nb = int(_chunk_ws(ctypes.byref(self.c), _np_ptr(lens)))
+            nb = _chunk_ws(ctypes.byref(self.c), arr)
             ws = torch.empty(nb, dtype=torch.uint8, device=self._dev) if nb > 0 else None
-        _check(_chunk_attn(_dptr(q), _row_stride(q), ctypes.byref(self.c), _np_ptr(lens), _dptr(out),
-                           _row_stride(out), _dptr(ws), ws.numel() if ws is not None else 0, _stream()),
-               "chunk_attn")
+        with _on(self._dev):
+            _check(_chunk_attn(_dptr(q), qs, ctypes.byref(self.c), arr, _dptr(out), os, _dptr(ws),
+                               ws.numel() if ws is not None else 0, _stream()), "chunk_attn")
         return out
 
     def quest_select(self, q, topk, out=None):
