@@ -624,6 +624,42 @@ typedef __attribute__((address_space(3))) f2 *LdsF2;
 constexpr int kFewWaves = 4;
 constexpr int kFewBuf = kSZBytes + P * D;  // an int8 record, the largest that is copied at once
 
+// The visits of a wavefront, 64 at a time: lane i holds the i-th.  Their table entries are read together
+// and handed out from registers; read one at a time each block waited for its own.
+struct Visits {
+  int level;
+  uint64_t k, v, drop;
+  __device__ __forceinline__ void read(const ChunkParams &p, const Job &j, int first, int stride, int v1, int lane) {
+    const int64_t at = first + (int64_t)lane * stride;
+    if (at >= v1) return;
+    if (at < j.nblk) {
+      const int64_t ti = j.u * p.nblk_cap + at;
+      level = p.level[ti];
+      k = (uint64_t)p.arena + p.koff[ti];
+      v = (uint64_t)p.arena + p.voff[ti];
+      drop = p.res_mask ? p.res_mask[ti] : 0;
+    } else {
+      const int r = (int)at - j.nblk, left = p.nres - r * P;
+      level = GKV_EXACT;
+      k = (uint64_t)(p.res_rows + (j.u * p.nrb_cap + r) * (2 * kExactBytes));
+      v = k + kExactBytes;
+      drop = left >= P ? 0 : ~0ull << left;
+    }
+  }
+  static __device__ __forceinline__ uint64_t lane64(uint64_t x, int i) {
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, i) |
+           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32;
+  }
+  __device__ __forceinline__ Visit at(int i) const {
+    Visit x;
+    x.level = __builtin_amdgcn_readlane(level, i);
+    x.k = (const uint8_t *)lane64(k, i);
+    x.v = (const uint8_t *)lane64(v, i);
+    x.drop = lane64(drop, i);
+    return x;
+  }
+};
+
 template <int CT>
 struct FewRows {
   f4 o[8][CT];  // O^T: register i of group c is channel 16 c + 4 kg + i
@@ -685,7 +721,10 @@ __device__ __forceinline__ void few_weights(uint32_t (&p)[CT][8], FewRows<CT> &r
 }
 
 // Copies of a record (exact: of its pages 2 half, 2 half + 1) to LDS, and how many they are.
-__device__ __forceinline__ void few_copy(const uint8_t *rec, int level, int half, uint32_t buf, int lane) {
+__device__ __forceinline__ void few_copy(const uint8_t *record, int level, int half, uint32_t buf, int lane) {
+  const uint8_t *rec = (const uint8_t *)(  // (the copies take their base from scalar registers)
+      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint64_t)record) |
+      (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)record >> 32)) << 32);
   if (level == GKV_EXACT) {
     const uint8_t *src = rec + half * (kExactBytes / 2);
 #pragma unroll
@@ -930,10 +969,12 @@ __global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(co
   // each level (in runs of blocks the ones with the exact blocks took a third longer)
   const int v1 = nvis, stride = split * kFewWaves;
   const uint32_t kbuf = lds + kQ + wave * 2 * kFewBuf, vbuf = kbuf + kFewBuf;
-  int at = j.part * kFewWaves + wave, half = 0;
+  int at = j.part * kFewWaves + wave, half = 0, nth = 0;
+  Visits batch = {};
   Visit x, next;
   if (at < v1) {
-    x = visit_at(p, j.u, at, j.nblk);
+    batch.read(p, j, at, stride, v1, lane);
+    x = batch.at(0);
     few_copy(x.k, x.level, 0, kbuf, lane);
   }
 #pragma unroll
@@ -957,7 +998,11 @@ __global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(co
     const bool again = x.level == GKV_EXACT && half == 0;  // the block's other half is next
     const int after = again ? at : at + stride;
     next = x;
-    if (!again && after < v1) next = visit_at(p, j.u, after, j.nblk);
+    if (!again && after < v1) {
+      nth = (nth + 1) & 63;
+      if (nth == 0) batch.read(p, j, after, stride, v1, lane);
+      next = batch.at(nth);
+    }
     const bool whole = whole_at(p, j, at, j.pos0);
     few_copy(x.v, x.level, half, vbuf, lane);
     few_wait(x.level);
