@@ -130,33 +130,54 @@ __device__ __forceinline__ void load_raw(Raw &x, const uint8_t *rec, int level, 
   }
 }
 
-// Codes 2 q and 2 q + 1 of a chunk, as fp16 (exact): their bits under a fixed exponent, less
-// the power of two that makes.
+// Codes 2 q and 2 q + 1 of a chunk under a fixed exponent, 2^k + code in fp16 (exact), and that
+// power of two; words 2 c and 2 c + 1 have the same one.
 template <int BITS>
-__device__ __forceinline__ half2v code_pair(const u4 (&w)[4], int q) {
-  uint32_t x, off;
+__device__ __forceinline__ uint32_t raw_offset(int q) {
+  if constexpr (BITS == 8) return 0x64006400u;
+  if constexpr (BITS == 4) return (q & 2) ? 0x64006400u : 0x54005400u;
+  const uint32_t e[4] = {0x44004400u, 0x4C004C00u, 0x54005400u, 0x64006400u};
+  return e[(q & 7) >> 1];
+}
+// The exponents in vector registers, behind the compiler's back: an and-or takes one constant that
+// is not in one, and as literals they make it two instructions.
+struct Exponents {
+  uint32_t e[4];  // 4, 16, 64, 1024
+  __device__ __forceinline__ Exponents() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      e[i] = raw_offset<2>(2 * i);
+      asm("" : "+v"(e[i]));
+    }
+  }
+};
+template <int BITS>
+__device__ __forceinline__ uint32_t raw_pair(const u4 (&w)[4], int q, const Exponents &x) {
   if constexpr (BITS == 8) {
-    x = __builtin_amdgcn_perm(0x64646464u, w[q >> 3][(q >> 1) & 3], (q & 1) ? 0x04030402u : 0x04010400u);
-    off = 0x64006400u;
+    return __builtin_amdgcn_perm(x.e[3], w[q >> 3][(q >> 1) & 3], (q & 1) ? 0x07030702u : 0x07010700u);
   } else if constexpr (BITS == 4) {
-    const uint32_t s = w[0][q >> 2] >> ((q & 1) ? 8 : 0);
-    x = (q & 2) ? (s & 0x000F000Fu) | 0x64006400u : (s & 0x00F000F0u) | 0x54005400u;
-    off = (q & 2) ? 0x64006400u : 0x54005400u;
+    const uint32_t y = w[0][q >> 2] >> ((q & 1) ? 8 : 0);
+    return (q & 2) ? (y & 0x000F000Fu) | x.e[3] : (y & 0x00F000F0u) | x.e[2];
   } else {
     const uint32_t y = w[0][q >> 3];
     switch (q & 7) {
-      case 0: case 1: x = ((q & 1 ? y >> 6 : y) & 0x03000300u) | (off = 0x44004400u); break;
-      case 2: case 3: x = ((q & 1 ? y >> 6 : y) & 0x00C000C0u) | (off = 0x4C004C00u); break;
-      case 4: case 5: x = ((q & 1 ? y >> 6 : y) & 0x00300030u) | (off = 0x54005400u); break;
-      case 6: x = (y & 0x00030003u) | (off = 0x64006400u); break;
-      default: x = (y & 0x000C000Cu) | (off = 0x5C005C00u); break;
+      case 0: case 1: return ((q & 1 ? y >> 6 : y) & 0x03000300u) | x.e[0];
+      case 2: case 3: return ((q & 1 ? y >> 6 : y) & 0x00C000C0u) | x.e[1];
+      case 4: case 5: return ((q & 1 ? y >> 6 : y) & 0x00300030u) | x.e[2];
+      default: return ((q & 1 ? y >> 2 : y) & 0x00030003u) | x.e[3];
     }
   }
+}
+// The codes alone.
+template <int BITS>
+__device__ __forceinline__ half2v code_pair(const u4 (&w)[4], int q, const Exponents &e) {
+  const uint32_t x = raw_pair<BITS>(w, q, e), off = raw_offset<BITS>(q);
   return __builtin_bit_cast(half2v, x) - __builtin_bit_cast(half2v, off);
 }
 
 typedef __attribute__((address_space(3))) u4 *LdsW4;
 typedef __attribute__((address_space(3))) u2 *LdsW2;
+typedef __attribute__((address_space(3))) uint32_t *LdsW1;
 
 // Scales and zeros in LDS: keys in the record's lane order (a lane's 32 are side by side);
 // values per channel as [channel & 15][channel >> 4], so that a lane's 8 are; values per
@@ -185,12 +206,12 @@ __device__ __forceinline__ uint32_t decoded(half2v code, uint32_t scale, uint32_
 }
 
 template <int BITS>
-__device__ __forceinline__ void stage_key_codes(uint32_t (&y)[16], const Raw &x, uint32_t head, int kg) {
+__device__ __forceinline__ void stage_key_codes(uint32_t (&y)[16], const Raw &x, uint32_t head, int kg, const Exponents &e) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const u4 s = ta::lds_u4(head + kg * 64 + j * 16), z = ta::lds_u4(head + 256 + kg * 64 + j * 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[4 * j + i] = decoded(code_pair<BITS>(x.w, 4 * j + i), s[i], z[i]);
+    for (int i = 0; i < 4; ++i) y[4 * j + i] = decoded(code_pair<BITS>(x.w, 4 * j + i, e), s[i], z[i]);
   }
 }
 __device__ __forceinline__ half2v twice(uint32_t pair, int i) {
@@ -201,20 +222,20 @@ __device__ __forceinline__ half2v twice(uint32_t pair, int i) {
 }
 template <int BITS>
 __device__ __forceinline__ void stage_value_codes(uint32_t (&y)[16], const Raw &x, uint32_t head, int pg, int lane,
-                                                  bool vtok) {
+                                                  bool vtok, const Exponents &e) {
   const int kg = lane >> 4, m = lane & 15;
   if (vtok) {  // tokens 16 pg + 4 kg .. + 3
     const u2 s = *(LdsW2)(uintptr_t)(head + 512 + (16 * pg + 4 * kg) * 2);
     const u2 z = *(LdsW2)(uintptr_t)(head + 512 + 128 + (16 * pg + 4 * kg) * 2);
 #pragma unroll
-    for (int q = 0; q < 16; ++q) y[q] = decoded(code_pair<BITS>(x.w, q), s[q & 1], z[q & 1]);
+    for (int q = 0; q < 16; ++q) y[q] = decoded(code_pair<BITS>(x.w, q, e), s[q & 1], z[q & 1]);
   } else {
     const u4 s = ta::lds_u4(head + 512 + m * 16), z = ta::lds_u4(head + 768 + m * 16);
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
       const int c = q >> 1;
       y[q] = __builtin_bit_cast(uint32_t,
-                                __builtin_elementwise_fma(code_pair<BITS>(x.w, q), twice(s[c >> 1], c & 1),
+                                __builtin_elementwise_fma(code_pair<BITS>(x.w, q, e), twice(s[c >> 1], c & 1),
                                                           twice(z[c >> 1], c & 1)));
     }
   }
@@ -222,9 +243,9 @@ __device__ __forceinline__ void stage_value_codes(uint32_t (&y)[16], const Raw &
 
 // A lane's key chunk of a page as fp16 pairs: words 4 j .. 4 j + 3 are channels 32 j + 8 kg .. + 7.
 template <int LEVEL>
-__device__ __forceinline__ void key_words(uint32_t (&y)[16], const Raw &x, uint32_t head, int kg) {
+__device__ __forceinline__ void key_words(uint32_t (&y)[16], const Raw &x, uint32_t head, int kg, const Exponents &e) {
   if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
-    stage_key_codes<LEVEL>(y, x, head, kg);
+    stage_key_codes<LEVEL>(y, x, head, kg, e);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = x.w[i >> 2][i & 3];
@@ -232,11 +253,12 @@ __device__ __forceinline__ void key_words(uint32_t (&y)[16], const Raw &x, uint3
 }
 
 // The same of any level.
-__device__ __forceinline__ void key_words_any(uint32_t (&y)[16], const Raw &x, int level, uint32_t head, int kg) {
-  if (level == GKV_INT8) key_words<GKV_INT8>(y, x, head, kg);
-  else if (level == GKV_INT4) key_words<GKV_INT4>(y, x, head, kg);
-  else if (level == GKV_INT2) key_words<GKV_INT2>(y, x, head, kg);
-  else key_words<GKV_EXACT>(y, x, head, kg);
+__device__ __forceinline__ void key_words_any(uint32_t (&y)[16], const Raw &x, int level, uint32_t head, int kg,
+                                              const Exponents &e) {
+  if (level == GKV_INT8) key_words<GKV_INT8>(y, x, head, kg, e);
+  else if (level == GKV_INT4) key_words<GKV_INT4>(y, x, head, kg, e);
+  else if (level == GKV_INT2) key_words<GKV_INT2>(y, x, head, kg, e);
+  else key_words<GKV_EXACT>(y, x, head, kg, e);
 }
 
 // A lane's value chunk of a centroid block: its channels' centroids, four to a channel, by the two
@@ -268,10 +290,10 @@ __device__ __forceinline__ void drop_words(uint32_t (&y)[16], uint64_t drop, int
 // (their weight is zero, but 0 * infinity is NaN).
 template <int LEVEL>
 __device__ __forceinline__ void value_words(uint32_t (&y)[16], const Raw &x, const uint8_t *rec, uint64_t drop,
-                                            uint32_t head, int pg, int lane, bool vtok) {
+                                            uint32_t head, int pg, int lane, bool vtok, const Exponents &e) {
   const int kg = lane >> 4;
   if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
-    stage_value_codes<LEVEL>(y, x, head, pg, lane, vtok);
+    stage_value_codes<LEVEL>(y, x, head, pg, lane, vtok, e);
   } else if constexpr (LEVEL == GKV_CENTROID) {
     centroid_words(y, x.w, table32(rec + KC * D * 2, pg) >> (8 * kg));
   } else if constexpr (LEVEL == GKV_MEAN) {
@@ -286,8 +308,8 @@ __device__ __forceinline__ void value_words(uint32_t (&y)[16], const Raw &x, con
 
 // The same of any level.
 __device__ __forceinline__ void value_words_any(uint32_t (&y)[16], const Raw &x, const Visit &v, uint32_t head, int pg,
-                                                int lane, bool vtok) {
-#define GKV_WORDS(lv) value_words<lv>(y, x, v.v, v.drop, head, pg, lane, vtok)
+                                                int lane, bool vtok, const Exponents &e) {
+#define GKV_WORDS(lv) value_words<lv>(y, x, v.v, v.drop, head, pg, lane, vtok, e)
   if (v.level == GKV_INT8) GKV_WORDS(GKV_INT8);
   else if (v.level == GKV_INT4) GKV_WORDS(GKV_INT4);
   else if (v.level == GKV_INT2) GKV_WORDS(GKV_INT2);
@@ -495,7 +517,8 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
   uint32_t y[16];
   load_raw<GKV_KEYS>(k, x.k, x.level, pg, lane);
   load_raw<GKV_VALUES>(w, x.v, x.level, pg, lane);
-  key_words_any(y, k, x.level, lds, kg);
+  const Exponents e;
+  key_words_any(y, k, x.level, lds, kg, e);
   if (drop >> (16 * pg + m) & 1)
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = 0;
@@ -504,7 +527,7 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
     *(u4 *)(tile + ta::key_place(16 * pg + m, 4 * j + kg)) = u4{y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]};
   Visit xd = x;
   xd.drop = drop;
-  value_words_any(y, w, xd, lds, pg, lane, p.vtok);
+  value_words_any(y, w, xd, lds, pg, lane, p.vtok, e);
   // operand form; two lanes' halves of a unit are exchanged, so that each stores 16 bytes: a lane
   // of the lower groups the units of even channel groups, its partner those of odd ones
   uint8_t *to = tile + ta::kTileBytes + pg * 4096 + (kg & 1) * 512 + m * 16;
@@ -784,12 +807,12 @@ __device__ __forceinline__ uint32_t lds_u16(uint32_t at) {
 
 // A lane's key chunk of page g: words 4 j .. 4 j + 3 are channels 32 j + 8 kg .. + 7.
 template <int LEVEL>
-__device__ __forceinline__ void few_key_words(uint32_t (&y)[16], uint32_t buf, int g, int lane) {
+__device__ __forceinline__ void few_key_words(uint32_t (&y)[16], uint32_t buf, int g, int lane, const Exponents &e) {
   const int kg = lane >> 4, m = lane & 15;
   if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
     Raw x;
     few_codes<LEVEL>(x, buf, g, lane);
-    stage_key_codes<LEVEL>(y, x, buf, kg);
+    stage_key_codes<LEVEL>(y, x, buf, kg, e);
   } else {
     uint32_t at = buf + g * 4096 + lane * 16, step = 1024;
     if constexpr (LEVEL == GKV_CENTROID) {
@@ -831,7 +854,7 @@ struct FewValues {
     }
   }
   // words 2 c and 2 c + 1: tokens 4 kg .. + 3 of page g, channel 16 c + m
-  __device__ __forceinline__ void words(uint32_t (&y)[16], uint32_t buf, int g, int lane, bool vtok) const {
+  __device__ __forceinline__ void words(uint32_t (&y)[16], uint32_t buf, int g, int lane, bool vtok, const Exponents &e) const {
     const int kg = lane >> 4;
     if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
       Raw x;
@@ -840,13 +863,13 @@ struct FewValues {
         const u2 s = *(LdsW2)(uintptr_t)(buf + (16 * g + 4 * kg) * 2);
         const u2 z = *(LdsW2)(uintptr_t)(buf + 128 + (16 * g + 4 * kg) * 2);
 #pragma unroll
-        for (int q = 0; q < 16; ++q) y[q] = decoded(code_pair<LEVEL>(x.w, q), s[q & 1], z[q & 1]);
+        for (int q = 0; q < 16; ++q) y[q] = decoded(code_pair<LEVEL>(x.w, q, e), s[q & 1], z[q & 1]);
       } else {
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
           const int c = q >> 1;
           y[q] = __builtin_bit_cast(uint32_t,
-                                    __builtin_elementwise_fma(code_pair<LEVEL>(x.w, q), twice(a[0][c >> 1], c & 1),
+                                    __builtin_elementwise_fma(code_pair<LEVEL>(x.w, q, e), twice(a[0][c >> 1], c & 1),
                                                               twice(a[1][c >> 1], c & 1)));
         }
       }
@@ -868,19 +891,26 @@ struct FewValues {
 // The operands of two pages of a copied record: keys, four a page; values, one for each 16
 // channels.  Only these depend on the level, so that the products' accumulators stand in no
 // branch (in one for each level they were copied from one to the next: 1100 moves).
-template <int LEVEL>
-__device__ __forceinline__ void few_key_pair(u4 (&a)[8], uint32_t buf, int pp, int lane) {
+template <int LEVEL, bool kRaw>
+__device__ __forceinline__ void few_keys(u4 (&a)[8], uint32_t buf, int pp, int lane, const Exponents &e) {
 #pragma unroll
   for (int g = 0; g < (LEVEL == GKV_MEAN ? 1 : 2); ++g) {
     uint32_t y[16];
-    few_key_words<LEVEL>(y, buf, 2 * pp + g, lane);
+    if constexpr (kRaw && (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2)) {
+      Raw x;
+      few_codes<LEVEL>(x, buf, 2 * pp + g, lane);
+#pragma unroll
+      for (int q = 0; q < 16; ++q) y[q] = raw_pair<LEVEL>(x.w, q, e);
+    } else {
+      few_key_words<LEVEL>(y, buf, 2 * pp + g, lane, e);
+    }
 #pragma unroll
     for (int d = 0; d < 4; ++d) a[4 * g + d] = u4{y[4 * d], y[4 * d + 1], y[4 * d + 2], y[4 * d + 3]};
   }
 }
-template <int LEVEL>
-__device__ __forceinline__ void few_value_pair(u4 (&a)[8], const Visit &x, int half, uint32_t buf, int pp, bool vtok,
-                                               int lane) {
+template <int LEVEL, bool kRaw>
+__device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half, uint32_t buf, int pp, bool vtok,
+                                           int lane, const Exponents &e) {
   if constexpr (LEVEL == GKV_MEAN) {  // the one key's place alone
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -888,18 +918,66 @@ __device__ __forceinline__ void few_value_pair(u4 (&a)[8], const Visit &x, int h
       a[c] = u4{lane < 16 ? v : 0, 0, 0, 0};
     }
   } else {
-    FewValues<LEVEL> v;
-    v.init(buf, lane, vtok);
     uint32_t y[2][16];
+    if (kRaw && (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) && !vtok) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      v.words(y[g], buf, 2 * pp + g, lane, vtok);
-      // a token that is read elsewhere has weight 0, but 0 * infinity is NaN (an integer
-      // block's infinities and NaN are those of whole channels)
-      if ((LEVEL == GKV_EXACT || LEVEL == GKV_CENTROID) && x.drop) drop_words(y[g], x.drop, 2 * (half + pp) + g, lane >> 4);
+      for (int g = 0; g < 2; ++g) {
+        Raw w;
+        few_codes<LEVEL>(w, buf, 2 * pp + g, lane);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) y[g][q] = raw_pair<LEVEL>(w.w, q, e);
+      }
+    } else {
+      FewValues<LEVEL> v;
+      v.init(buf, lane, vtok);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        v.words(y[g], buf, 2 * pp + g, lane, vtok, e);
+        // a token that is read elsewhere has weight 0, but 0 * infinity is NaN (an integer
+        // block's infinities and NaN are those of whole channels)
+        if ((LEVEL == GKV_EXACT || LEVEL == GKV_CENTROID) && x.drop)
+          drop_words(y[g], x.drop, 2 * (half + pp) + g, lane >> 4);
+      }
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c) a[c] = u4{y[0][2 * c], y[0][2 * c + 1], y[1][2 * c], y[1][2 * c + 1]};
+  }
+}
+
+// With one row tile the scales and zeros of an integer block stay out of its codes' operands, which
+// are 2^k + code as they come from the bits (for four tiles that is more work, not less):
+//   q . k = sum (2^k + code) (q s) + sum z q - sum 2^k (q s), with q s as two fp16 terms and the
+//   constant part from the matrix units too, for any token the same;
+//   sum p v = s (sum p (2^k + code) - 2^k sum p) + z sum p, once a block.
+// Both sums are held in 32 bits, where 2^k <= 1024 costs 2^-14 of a code's step at most.  The rows of
+// q are brought below 1 and s is at most 65504 2 / 3 (two bits), 8734 or 514, so that no q s
+// overflows; those of eight bits are raised by 2^6, so that the second term of one is lost only
+// where 2^-12 of the code's span is less than a step of fp16's smallest numbers.
+constexpr float kRaise = 64.f;
+template <int LEVEL>
+__device__ __forceinline__ void few_fold(u4 (&hi)[4], u4 (&lo)[4], f4 &start, f4 &zero, uint32_t buf, uint32_t lds,
+                                         int lane) {
+  const int kg = lane >> 4;
+  start = zero = f4{0.f, 0.f, 0.f, 0.f};
+  half2v raise;
+  raise[0] = raise[1] = (_Float16)kRaise;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const u4 q = ta::lds_u4(lds + d * 1024 + lane * 16), sc = ta::lds_u4(buf + kg * 64 + d * 16);
+    u4 off;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      half2v s = halves(sc[i]);
+      if (LEVEL == GKV_INT8) s *= raise;
+      const half2v x = halves(q[i]) * s;
+      hi[d][i] = __builtin_bit_cast(uint32_t, x);
+      lo[d][i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(halves(q[i]), s, -x));
+      off[i] = raw_offset<LEVEL>(4 * d + i) | 0x80008000u;
+    }
+    f4 &z = LEVEL == GKV_INT8 ? zero : start;
+    z = mfma16(ta::lds_u4(buf + 256 + kg * 64 + d * 16), q, z);
+    start = mfma16(off, hi[d], start);
+    start = mfma16(off, lo[d], start);
   }
 }
 
@@ -941,22 +1019,24 @@ __device__ __forceinline__ void few_odd(u4 (&odd)[CT], const uint64_t (&vis)[CT]
   }
 }
 
-#define GKV_LEVELS(level, f, ...)                                \
-  do {                                                           \
-    if (level == GKV_INT4) f<GKV_INT4>(__VA_ARGS__);             \
-    else if (level == GKV_INT2) f<GKV_INT2>(__VA_ARGS__);        \
-    else if (level == GKV_INT8) f<GKV_INT8>(__VA_ARGS__);        \
-    else if (level == GKV_EXACT) f<GKV_EXACT>(__VA_ARGS__);      \
-    else if (level == GKV_CENTROID) f<GKV_CENTROID>(__VA_ARGS__); \
-    else f<GKV_MEAN>(__VA_ARGS__);                               \
+#define GKV_LEVELS(level, f, raw, ...)                               \
+  do {                                                                \
+    if (level == GKV_INT4) f<GKV_INT4, raw>(__VA_ARGS__);             \
+    else if (level == GKV_INT2) f<GKV_INT2, raw>(__VA_ARGS__);        \
+    else if (level == GKV_INT8) f<GKV_INT8, raw>(__VA_ARGS__);        \
+    else if (level == GKV_EXACT) f<GKV_EXACT, raw>(__VA_ARGS__);      \
+    else if (level == GKV_CENTROID) f<GKV_CENTROID, raw>(__VA_ARGS__); \
+    else f<GKV_MEAN, raw>(__VA_ARGS__);                               \
   } while (0)
 
 template <int CT>
 __global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(const ChunkParams p) {
   constexpr int kR = 16 * CT;
-  // the queries' operands, then each wavefront's two buffers; in the end its state
+  constexpr bool kFold = CT == 1;
+  // the queries' operands, then each wavefront's two buffers, the rows' largest; in the end the
+  // wavefronts' states
   constexpr int kQ = CT * 4096;
-  __shared__ __align__(16) uint8_t sh[kQ + kFewWaves * 2 * kFewBuf];
+  __shared__ __align__(16) uint8_t sh[kQ + kFewWaves * 2 * kFewBuf + (kFold ? kFewWaves * 64 : 0)];
   static_assert((8 * 4 + 2) * CT * 256 * 2 <= sizeof(sh), "two wavefronts' states");
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)sh;
   const Job j = job_of(p, kR);
@@ -977,12 +1057,33 @@ __global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(co
     x = batch.at(0);
     few_copy(x.k, x.level, 0, kbuf, lane);
   }
+  float sl2 = p.sl2;
 #pragma unroll
   for (int t = 0; t < CT; ++t) {  // a wavefront copies channels 32 wave .. + 31
     const int rc = min(16 * t + m, j.rows - 1), tok = rc / p.G, g = rc - tok * p.G;
-    *(LdsW4)(uintptr_t)(lds + (t * 4 + wave) * 1024 + lane * 16) =
-        *(const u4 *)(p.q + (j.row0 + tok) * p.qs + (int64_t)(j.h * p.G + g) * D + 8 * kg + 32 * wave);
+    u4 q = *(const u4 *)(p.q + (j.row0 + tok) * p.qs + (int64_t)(j.h * p.G + g) * D + 8 * kg + 32 * wave);
+    if constexpr (kFold) {
+      // times the power of two that brings the row's largest below 1: a scale is at most
+      // 65504 2 / 3, so that their product is finite
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max(q[i] & 0x7FFFu, q[i] >> 16 & 0x7FFFu));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+      const uint32_t tops = lds + kQ + kFewWaves * 2 * kFewBuf;
+      if (lane < 16) *(LdsW1)(uintptr_t)(tops + (wave * 16 + m) * 4) = top;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kFewWaves; ++i) top = max(top, *(LdsW1)(uintptr_t)(tops + (i * 16 + m) * 4));
+      const int k = top == 0 || top >= T16::kInf ? 0 : 14 - (int)(top >> 10);
+      const uint32_t f = (k >= -14 ? (15 + k) << 10 : 0x400 >> (-14 - k)) * 0x10001u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = __builtin_bit_cast(uint32_t, halves(q[i]) * halves(f));
+      sl2 = ldexpf(sl2, -k);
+    }
+    *(LdsW4)(uintptr_t)(lds + (t * 4 + wave) * 1024 + lane * 16) = q;
   }
+  const Exponents e;
   FewRows<CT> r;
   u4 odd[CT];
 #pragma unroll
@@ -1008,34 +1109,57 @@ __global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(co
     few_wait(x.level);
     const bool two = x.level != GKV_EXACT && x.level != GKV_MEAN;  // pairs of pages
     f4 s[4][CT];
+    const bool codes = x.level == GKV_INT8 || x.level == GKV_INT4 || x.level == GKV_INT2;
+    u4 hi[4], lo[4];
+    f4 start = {0.f, 0.f, 0.f, 0.f}, zero;
+    if constexpr (kFold) {
+      if (x.level == GKV_INT4) few_fold<GKV_INT4>(hi, lo, start, zero, kbuf, lds, lane);
+      else if (x.level == GKV_INT2) few_fold<GKV_INT2>(hi, lo, start, zero, kbuf, lds, lane);
+      else if (x.level == GKV_INT8) few_fold<GKV_INT8>(hi, lo, start, zero, kbuf, lds, lane);
+      else
+#pragma unroll
+        for (int d = 0; d < 4; ++d) hi[d] = ta::lds_u4(lds + d * 1024 + lane * 16);
+    }
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp) {
       if (pp == 0 || two) {
         u4 a[8];
-        GKV_LEVELS(x.level, few_key_pair, a, kbuf, pp, lane);
+        GKV_LEVELS(x.level, few_keys, kFold, a, kbuf, pp, lane, e);
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
-          s[2 * pp][t] = s[2 * pp + 1][t] = f4{0.f, 0.f, 0.f, 0.f};
+          s[2 * pp][t] = s[2 * pp + 1][t] = start;
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
-            const u4 q = ta::lds_u4(lds + (t * 4 + d) * 1024 + lane * 16);
+            const u4 q = kFold ? hi[d] : ta::lds_u4(lds + (t * 4 + d) * 1024 + lane * 16);
 #pragma unroll
             for (int g = 0; g < 2; ++g) s[2 * pp + g][t] = mfma16(a[4 * g + d], q, s[2 * pp + g][t]);
           }
+          if (kFold && codes)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+              for (int g = 0; g < 2; ++g) s[2 * pp + g][t] = mfma16(a[4 * g + d], lo[d], s[2 * pp + g][t]);
         }
-      } else {
-#pragma unroll
-        for (int t = 0; t < CT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[2][t][i] = s[3][t][i] = -__builtin_inff();
       }
-      asm volatile("" ::: "memory");
+      if (!kFold) asm volatile("" ::: "memory");  // the queries' operands are read again (kept, they spill)
+    }
+    if (kFold && x.level == GKV_INT8) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[g][0][i] = __builtin_fmaf(s[g][0][i], 1.f / kRaise, zero[i]);
+    }
+    if (!two) {
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[2][t][i] = s[3][t][i] = -__builtin_inff();
     }
     if (x.level == GKV_MEAN) {
       // one key stands for all the block's tokens: its weight times their number, in the first
       // group's first place alone
       const int n = P - __popcll(x.drop);
-      const float more = __builtin_amdgcn_logf((float)n) / p.sl2, no = -__builtin_inff();
+      const float more = __builtin_amdgcn_logf((float)n) / sl2, no = -__builtin_inff();
 #pragma unroll
       for (int t = 0; t < CT; ++t) {
         s[0][t][0] = lane < 16 && n ? s[0][t][0] + more : no;
@@ -1059,20 +1183,60 @@ __global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(co
       }
     }
     uint32_t w[CT][8];
-    few_weights<CT>(w, r, s, p.sl2);
+    few_weights<CT>(w, r, s, sl2);
     few_wait(after < v1 ? next.level : -1);
     if (!whole) few_odd<CT>(odd, vis, vbuf, half, lane);  // an exact block (the host sees to it)
+    const bool scaled = kFold && codes && !p.vtok;
+    f4 acc[kFold ? 8 : 1];
+    float sum = 0.f;  // of the step's weights
+    if constexpr (kFold) {
+      if (scaled) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = T16::add2(w[0][i], sum);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+      }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint32_t off = x.level == GKV_INT8   ? raw_offset<8>(2 * c)
+                             : x.level == GKV_INT4 ? raw_offset<4>(2 * c)
+                                                   : raw_offset<2>(2 * c);
+        const float z = scaled ? -(float)halves(off)[0] * sum : 0.f;
+        acc[c] = f4{z, z, z, z};
+      }
+    }
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp)
       if (pp == 0 || two) {
         u4 a[8];
-        GKV_LEVELS(x.level, few_value_pair, a, x, half, vbuf, pp, p.vtok, lane);
+        GKV_LEVELS(x.level, few_values, kFold, a, x, half, vbuf, pp, p.vtok, lane, e);
 #pragma unroll
         for (int c = 0; c < 8; ++c)
 #pragma unroll
-          for (int t = 0; t < CT; ++t)
-            r.o[c][t] = mfma16(a[c], u4{w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]}, r.o[c][t]);
+          for (int t = 0; t < CT; ++t) {
+            const u4 b = {w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]};
+            if constexpr (kFold) acc[c] = mfma16(a[c], b, acc[c]);
+            else r.o[c][t] = mfma16(a[c], b, r.o[c][t]);
+          }
       }
+    if constexpr (kFold) {
+      // channels 16 c + 4 kg .. + 3 lie side by side in the header's lane order
+      if (scaled) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const u4 sc = ta::lds_u4(vbuf + kg * 64 + h * 16), z = ta::lds_u4(vbuf + 256 + kg * 64 + h * 16);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            f4 &o = r.o[2 * h + (i >> 2)][0];
+            const float y = __builtin_fmaf((float)halves(sc[i >> 1])[i & 1], acc[2 * h + (i >> 2)][i & 3], o[i & 3]);
+            o[i & 3] = __builtin_fmaf((float)halves(z[i >> 1])[i & 1], sum, y);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) r.o[c][0] += acc[c];
+      }
+    }
     few_read();
     x = next;
     half = again;
@@ -1083,11 +1247,13 @@ __global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(co
   for (int t = 0; t < CT; ++t) {
     r.l[t] += __shfl_xor(r.l[t], 16);
     r.l[t] += __shfl_xor(r.l[t], 32);
+    if (__any(odd[t][0] | odd[t][1] | odd[t][2] | odd[t][3]))  // the values that stayed out of the products
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {  // the values that stayed out of the products
-      const uint32_t b = odd[t][i >> 3] >> (8 * (i >> 2 & 1) + 2 * (i & 3)) & 3u;
-      r.o[i >> 2][t][i & 3] += b == 0 ? 0.f : b == 3 ? __builtin_nanf("") : b == 1 ? __builtin_inff() : -__builtin_inff();
-    }
+      for (int i = 0; i < 32; ++i) {
+        const uint32_t b = odd[t][i >> 3] >> (8 * (i >> 2 & 1) + 2 * (i & 3)) & 3u;  // 0, infinity, -infinity, NaN
+        const uint32_t v = (b & 1u ? 0x7F800000u : b ? 0xFF800000u : 0u) | (b == 3 ? 0x400000u : 0u);
+        r.o[i >> 2][t][i & 3] += __builtin_bit_cast(float, v);
+      }
   }
 #pragma unroll
   for (int n = 2; n >= 1; n >>= 1) {

@@ -55,11 +55,14 @@ def mixed_levels(T):
 class Case:
     """A cache of lens tokens and the rows that are appended to it."""
 
-    def __init__(self, gpu, seed, lens, news, Hq, Hkv, prof="tiny", page=0, vtok=False, nres=0, ragged=True, slack=0):
+    def __init__(self, gpu, seed, lens, news, Hq, Hkv, prof="tiny", page=0, vtok=False, nres=0, ragged=True, slack=0,
+                 scale=1.0):
         self.lens, self.news, self.Hq, self.Hkv, self.G = list(lens), list(news), Hq, Hkv, Hq // Hkv
         B, T = len(lens), max(1, max(lens))
         self.end = [max(t, 0) + n for t, n in zip(lens, news)]
         self.ks, self.vs = kv_all(seed, B, Hkv, max(self.end))
+        if scale != 1.0:
+            self.ks, self.vs = (ofp16.from_f64(ofp16.to_f64(x) * scale) for x in (self.ks, self.vs))
         lv = level_table(lens, Hkv, prof)
         opened = sum(-(-e // 64) - -(-max(t, 0) // 64) for e, t in zip(self.end, lens)) * Hkv
         self.cache = gpu.GradedCache.build(
@@ -276,6 +279,34 @@ def test_long_contexts_are_split(gpu, prof, T, n):
     """More workgroups than row tiles: partials over the context, joined."""
     c = Case(gpu, 53, (T, 200), (n, 1), 8, 2, prof)
     c.check(c.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,n", [(1, 15), (1, 16), (1, 17), (1, 31), (1, 32), (1, 33), (1, 48), (1, 49), (1, 64), (1, 65),
+                                  (4, 4), (4, 5), (7, 2), (7, 3), (5, 9), (5, 13), (16, 4), (16, 5)])
+@pytest.mark.parametrize("vtok,nres", [(False, 0), (True, 70)])
+def test_row_counts(gpu, Hq, n, vtok, nres):
+    """Rows about every bound of a row tile, over all six levels (the newest rows exact: the
+    few-row form; see test_rows_in_demoted_blocks for the other)."""
+    T = 64 * 40 + 5
+    c = Case(gpu, 73, (T,), (n,), Hq, 1, mixed_levels, vtok=vtok, nres=nres, ragged=False)
+    c.check(c.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 3, 40, 100])
+@pytest.mark.parametrize("prof", [mixed_levels, "exact"])
+def test_queries_of_all_sizes(gpu, n, prof):
+    """Rows scaled by 2^-14 .. 2^12, rows of zeros, and keys and values near the ends of fp16."""
+    c = Case(gpu, 75, (64 * 25,), (n,), 4, 1, prof)
+    size = np.exp2(np.resize([-14, 12, 0, -7, 5, -20, 9], n * 4)).reshape(n, 4, 1)
+    size[n // 2, 1] = 0.0
+    c.q = (c.q.astype(np.float64) * size).astype(np.float16)
+    c.check(c.run())
+    for scale in (2.0 ** 10, 2.0 ** -10):
+        d = Case(gpu, 75, (64 * 25,), (n,), 4, 1, prof, scale=scale)
+        d.q = (d.q.astype(np.float64) / scale).astype(np.float16)
+        d.check(d.run())
 
 
 @pytest.mark.gpu
