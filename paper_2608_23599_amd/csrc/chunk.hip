@@ -3,8 +3,8 @@
 // dense decode read.
 //
 // Two ways, chosen for each sequence by its rows (tokens times heads of a group):
-//  * few rows: every wavefront holds all of a (sequence, KV head)'s rows, reads whole blocks of its
-//    own straight from the records into operands, and decodes them there;
+//  * few rows: every wavefront holds 16 of a (sequence, KV head)'s rows, copies blocks of its own
+//    to LDS and decodes them into operands;
 //  * many rows: the cache is decoded once to fp16 tiles in the workspace, over which row tiles
 //    go as a prompt's do (tile_attn.h).
 // Either splits a long context over workgroups whose partials a merge kernel joins.  A graded
@@ -627,25 +627,35 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams 
 }
 
 // ---------------------------------------------------------------- few rows
-// At most 16 CT rows of a (sequence, KV head): every wavefront holds all of them and reads blocks of
-// its own.  The records are laid out for 16x16x32 MFMA (a lane's key chunk is the four
-// operands of its page, its value chunk of two pages the eight operands of 32 tokens), and
-// the scores' layout (lane l: row l & 15, token 16 page + 4 (l >> 4) + i) is the second
-// product's operand layout again.
+// Row tiles of 16: every wavefront holds one and reads blocks of its own.  The records are laid out
+// for 16x16x32 MFMA (a lane's key chunk is the four operands of its page, its value chunk of two
+// pages the eight operands of 32 tokens), and the scores' layout (lane l: row l & 15, token 16
+// page + 4 (l >> 4) + i) is the second product's operand layout again.
 //
-// A record is copied to LDS as it is (asynchronous copies, 16 bytes a lane, with an exact or int8
-// chunk's pieces one behind the other so that a read finds each bank once) and decoded from
-// there: the copies hold no registers, so that two wavefronts fit a SIMD and a record is
-// always on its way.  A step is a block, or half an exact one; its values are copied from
-// the start of its key product on, the next step's keys from the end of that.  No other
-// vector memory instruction runs in the loop, so the wait for a record is a constant count.
+// The records are copied to LDS as they are (asynchronous copies, 16 bytes a lane, with an exact or
+// int8 chunk's pieces one behind the other so that a read finds each bank once) and decoded
+// from there: the copies hold no registers, so that two wavefronts fit a SIMD.  A step is a
+// block, or half an exact one; its values are copied from the start of its key product on,
+// the next step's keys from the end of that.  No other vector memory instruction runs in the
+// loop (but every 64 blocks), so the wait for a copy is a constant count.
+//
+// The scales and zeros of an integer block stay out of its codes' operands, which are 2^k + code as
+// they come from the bits:
+//   q . k = sum (2^k + code) (q s) + sum z q - sum 2^k (q s), with q s as two fp16 terms and the
+//   constant part from the matrix units too, for any token the same;
+//   sum p v = s (sum p (2^k + code) - 2^k sum p) + z sum p, once a step.
+// Both sums are held in 32 bits, where 2^k <= 1024 costs 2^-14 of a code's step at most.  The rows of
+// q are brought below 1 and s is at most 65504 2 / 3 (two bits), 8734 or 514, so that no q s
+// overflows; those of eight bits are raised by 2^6, so that the second term of one is lost only
+// where 2^-12 of the code's span is less than a step of fp16's smallest numbers.
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) f4 *LdsF4;
 typedef __attribute__((address_space(3))) f2 *LdsF2;
 
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = 4, kFewRows = 16;
 constexpr int kFewBuf = kSZBytes + P * D;  // an int8 record, the largest that is copied at once
+constexpr float kRaise = 64.f;
 
 // The visits of a wavefront, 64 at a time: lane i holds the i-th.  Their table entries are read together
 // and handed out from registers; read one at a time each block waited for its own.
@@ -683,10 +693,9 @@ struct Visits {
   }
 };
 
-template <int CT>
 struct FewRows {
-  f4 o[8][CT];  // O^T: register i of group c is channel 16 c + 4 kg + i
-  float m[CT], raise[CT], l[CT];
+  f4 o[8];  // O^T: register i of group c is channel 16 c + 4 kg + i
+  float m, raise, l;
 };
 
 __device__ __forceinline__ f4 mfma16(u4 a, u4 b, f4 c) {
@@ -700,50 +709,34 @@ __device__ __forceinline__ float over_groups(float x) {  // the maximum over a r
 }
 
 // Scores to packed probabilities (two words a page), raising the maxima as tile_attn.h does.
-template <int CT>
-__device__ __forceinline__ void few_weights(uint32_t (&p)[CT][8], FewRows<CT> &r, const f4 (&s)[4][CT], float sl2) {
-  float top[CT];
-  bool go = false;
+__device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, const f4 (&s)[4], float sl2) {
+  float top = -__builtin_inff();
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    top[t] = -__builtin_inff();
+  for (int g = 0; g < 4; ++g)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, __builtin_fmaf(s[g][i], sl2, -r.m));
+  if (__builtin_expect(__any(top > r.raise), 0)) {
+    const float high = over_groups(top);
+    const bool mine = high > r.raise;
+    const float up = mine ? high : 0.f;
+    const float f = r.raise < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
+    r.raise = mine ? ta::kRescale : r.raise;
+    r.m += up;
+    r.l *= f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], __builtin_fmaf(s[g][t][i], sl2, -r.m[t]));
-    go |= top[t] > r.raise[t];
+    for (int c = 0; c < 8; ++c) r.o[c] *= f;
   }
-  if (__builtin_expect(__any(go), 0)) {
 #pragma unroll
-    for (int t = 0; t < CT; ++t) {
-      const float high = over_groups(top[t]);
-      const bool mine = high > r.raise[t];
-      const float up = mine ? high : 0.f;
-      const float f = r.raise[t] < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
-      r.raise[t] = mine ? ta::kRescale : r.raise[t];
-      r.m[t] += up;
-      r.l[t] *= f;
+  for (int g = 0; g < 4; ++g)
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.o[c][t][i] *= f;
+    for (int i = 0; i < 2; ++i) {
+      const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * i], sl2, -r.m));
+      const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * i + 1], sl2, -r.m));
+      p[2 * g + i] = T16::pack(a, b);
     }
-  }
-#pragma unroll
-  for (int t = 0; t < CT; ++t)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][t][2 * i], sl2, -r.m[t]));
-        const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][t][2 * i + 1], sl2, -r.m[t]));
-        const uint32_t w = T16::pack(a, b);
-        p[t][2 * g + i] = w;
-        r.l[t] = T16::add2(w, r.l[t]);
-      }
 }
 
-// Copies of a record (exact: of its pages 2 half, 2 half + 1) to LDS, and how many they are.
+// Copies of a record (exact: of its pages 2 half, 2 half + 1) to LDS.
 __device__ __forceinline__ void few_copy(const uint8_t *record, int level, int half, uint32_t buf, int lane) {
   const uint8_t *rec = (const uint8_t *)(  // (the copies take their base from scalar registers)
       (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint64_t)record) |
@@ -783,10 +776,14 @@ __device__ __forceinline__ void few_wait(int level) {
   else if (level == GKV_MEAN) asm volatile("s_waitcnt vmcnt(1)" ::: "memory");
   else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
-// LDS reads of the buffer that is copied over next have returned.
+// LDS reads of what is copied over next have returned.
 __device__ __forceinline__ void few_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// The codes of a lane's chunk of page g in a copied record.
+__device__ __forceinline__ uint32_t lds_u16(uint32_t at) {
+  return *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)at;
+}
+
+// The codes of a lane's chunk of page g.
 template <int BITS>
 __device__ __forceinline__ void few_codes(Raw &x, uint32_t buf, int g, int lane) {
   const uint32_t at = buf + kSZBytes;
@@ -801,159 +798,86 @@ __device__ __forceinline__ void few_codes(Raw &x, uint32_t buf, int g, int lane)
     x.w[0][1] = y[1];
   }
 }
-__device__ __forceinline__ uint32_t lds_u16(uint32_t at) {
-  return *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)at;
-}
 
-// A lane's key chunk of page g: words 4 j .. 4 j + 3 are channels 32 j + 8 kg .. + 7.
-template <int LEVEL>
-__device__ __forceinline__ void few_key_words(uint32_t (&y)[16], uint32_t buf, int g, int lane, const Exponents &e) {
-  const int kg = lane >> 4, m = lane & 15;
-  if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
-    Raw x;
-    few_codes<LEVEL>(x, buf, g, lane);
-    stage_key_codes<LEVEL>(y, x, buf, kg, e);
-  } else {
-    uint32_t at = buf + g * 4096 + lane * 16, step = 1024;
-    if constexpr (LEVEL == GKV_CENTROID) {
-      const uint32_t ids = *(__attribute__((address_space(3))) const uint32_t *)(uintptr_t)(buf + KC * D * 2 + 4 * g);
-      at = buf + (ids >> (2 * m) & 3u) * (D * 2) + 16 * kg;
-      step = 64;
-    } else if constexpr (LEVEL == GKV_MEAN) {
-      at = buf + 16 * kg;
-      step = 64;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const u4 a = ta::lds_u4(at + j * step);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[4 * j + i] = a[i];
-    }
-  }
-}
+constexpr bool is_codes(int level) { return level == GKV_INT8 || level == GKV_INT4 || level == GKV_INT2; }
 
-// What the values of a copied record are decoded with: scales and zeros (per channel: of the
-// lane's eight, channel 16 c + m in half c & 1 of word c >> 1), or a centroid block's rows.
-template <int LEVEL>
-struct FewValues {
-  u4 a[LEVEL == GKV_CENTROID ? 4 : 2];
-  __device__ __forceinline__ void init(uint32_t buf, int lane, bool vtok) {
-    const int m = lane & 15;
-    if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
-      if (!vtok)
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {  // entry 32 (m >> 2) + 4 c + (m & 3) holds channel 16 c + m
-            const uint32_t at = buf + 256 * k + 2 * (32 * (m >> 2) + (m & 3)) + 16 * c;
-            a[k][c] = lds_u16(at) | lds_u16(at + 8) << 16;
-          }
-    } else if constexpr (LEVEL == GKV_CENTROID) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = ta::lds_u4(buf + m * 64 + 16 * i);
-    }
-  }
-  // words 2 c and 2 c + 1: tokens 4 kg .. + 3 of page g, channel 16 c + m
-  __device__ __forceinline__ void words(uint32_t (&y)[16], uint32_t buf, int g, int lane, bool vtok, const Exponents &e) const {
-    const int kg = lane >> 4;
-    if constexpr (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) {
-      Raw x;
-      few_codes<LEVEL>(x, buf, g, lane);
-      if (vtok) {
-        const u2 s = *(LdsW2)(uintptr_t)(buf + (16 * g + 4 * kg) * 2);
-        const u2 z = *(LdsW2)(uintptr_t)(buf + 128 + (16 * g + 4 * kg) * 2);
-#pragma unroll
-        for (int q = 0; q < 16; ++q) y[q] = decoded(code_pair<LEVEL>(x.w, q, e), s[q & 1], z[q & 1]);
-      } else {
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const int c = q >> 1;
-          y[q] = __builtin_bit_cast(uint32_t,
-                                    __builtin_elementwise_fma(code_pair<LEVEL>(x.w, q, e), twice(a[0][c >> 1], c & 1),
-                                                              twice(a[1][c >> 1], c & 1)));
-        }
-      }
-    } else if constexpr (LEVEL == GKV_CENTROID) {
-      const uint32_t ids =
-          *(__attribute__((address_space(3))) const uint32_t *)(uintptr_t)(buf + KC * D * 2 + 4 * g) >> (8 * kg);
-      centroid_words(y, a, ids);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u4 b = ta::lds_u4(buf + g * 4096 + j * 1024 + lane * 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[4 * j + i] = b[i];
-      }
-    }
-  }
-};
-
-// The operands of two pages of a copied record: keys, four a page; values, one for each 16
+// The operands of pages 2 pp and 2 pp + 1 (exact: of the half's two): keys, four a page; values, one for each 16
 // channels.  Only these depend on the level, so that the products' accumulators stand in no
 // branch (in one for each level they were copied from one to the next: 1100 moves).
-template <int LEVEL, bool kRaw>
+template <int LEVEL>
 __device__ __forceinline__ void few_keys(u4 (&a)[8], uint32_t buf, int pp, int lane, const Exponents &e) {
+  const int kg = lane >> 4, m = lane & 15;
 #pragma unroll
   for (int g = 0; g < (LEVEL == GKV_MEAN ? 1 : 2); ++g) {
-    uint32_t y[16];
-    if constexpr (kRaw && (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2)) {
+    if constexpr (is_codes(LEVEL)) {
       Raw x;
       few_codes<LEVEL>(x, buf, 2 * pp + g, lane);
 #pragma unroll
-      for (int q = 0; q < 16; ++q) y[q] = raw_pair<LEVEL>(x.w, q, e);
+      for (int q = 0; q < 16; ++q) a[4 * g + (q >> 2)][q & 3] = raw_pair<LEVEL>(x.w, q, e);
     } else {
-      few_key_words<LEVEL>(y, buf, 2 * pp + g, lane, e);
-    }
+      uint32_t at = buf + (LEVEL == GKV_EXACT ? g * 4096 + lane * 16 : kg * 16);
+      if constexpr (LEVEL == GKV_CENTROID)
+        at += (*(LdsW1)(uintptr_t)(buf + KC * D * 2 + 4 * (2 * pp + g)) >> (2 * m) & 3u) * (D * 2);
 #pragma unroll
-    for (int d = 0; d < 4; ++d) a[4 * g + d] = u4{y[4 * d], y[4 * d + 1], y[4 * d + 2], y[4 * d + 3]};
+      for (int j = 0; j < 4; ++j) a[4 * g + j] = ta::lds_u4(at + j * (LEVEL == GKV_EXACT ? 1024 : 64));
+    }
   }
 }
-template <int LEVEL, bool kRaw>
+template <int LEVEL>
 __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half, uint32_t buf, int pp, bool vtok,
                                            int lane, const Exponents &e) {
+  const int kg = lane >> 4, m = lane & 15;
+  uint32_t y[2][16];
   if constexpr (LEVEL == GKV_MEAN) {  // the one key's place alone
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-      const uint32_t v = lds_u16(buf + 2 * (16 * c + (lane & 15)));
+      const uint32_t v = lds_u16(buf + 2 * (16 * c + m));
       a[c] = u4{lane < 16 ? v : 0, 0, 0, 0};
     }
-  } else {
-    uint32_t y[2][16];
-    if (kRaw && (LEVEL == GKV_INT8 || LEVEL == GKV_INT4 || LEVEL == GKV_INT2) && !vtok) {
+    return;
+  } else if constexpr (is_codes(LEVEL)) {
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        Raw w;
-        few_codes<LEVEL>(w, buf, 2 * pp + g, lane);
+    for (int g = 0; g < 2; ++g) {
+      Raw w;
+      few_codes<LEVEL>(w, buf, 2 * pp + g, lane);
 #pragma unroll
-        for (int q = 0; q < 16; ++q) y[g][q] = raw_pair<LEVEL>(w.w, q, e);
-      }
-    } else {
-      FewValues<LEVEL> v;
-      v.init(buf, lane, vtok);
+      for (int q = 0; q < 16; ++q) y[g][q] = raw_pair<LEVEL>(w.w, q, e);
+      if (vtok) {  // scales of tokens: into the values here
+        const uint32_t at = buf + (16 * (2 * pp + g) + 4 * kg) * 2;
+        const u2 s = *(LdsW2)(uintptr_t)at, z = *(LdsW2)(uintptr_t)(at + 128);
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        v.words(y[g], buf, 2 * pp + g, lane, vtok, e);
-        // a token that is read elsewhere has weight 0, but 0 * infinity is NaN (an integer
-        // block's infinities and NaN are those of whole channels)
-        if ((LEVEL == GKV_EXACT || LEVEL == GKV_CENTROID) && x.drop)
-          drop_words(y[g], x.drop, 2 * (half + pp) + g, lane >> 4);
+        for (int q = 0; q < 16; ++q)
+          y[g][q] = decoded(halves(y[g][q]) - halves(raw_offset<LEVEL>(q)), s[q & 1], z[q & 1]);
       }
     }
+  } else {
+    u4 cent[4];
+    if constexpr (LEVEL == GKV_CENTROID)
 #pragma unroll
-    for (int c = 0; c < 8; ++c) a[c] = u4{y[0][2 * c], y[0][2 * c + 1], y[1][2 * c], y[1][2 * c + 1]};
+      for (int i = 0; i < 4; ++i) cent[i] = ta::lds_u4(buf + m * 64 + 16 * i);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if constexpr (LEVEL == GKV_CENTROID) {
+        centroid_words(y[g], cent, *(LdsW1)(uintptr_t)(buf + KC * D * 2 + 4 * (2 * pp + g)) >> (8 * kg));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const u4 b = ta::lds_u4(buf + g * 4096 + j * 1024 + lane * 16);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[g][4 * j + i] = b[i];
+        }
+      }
+      // a token that is read elsewhere has weight 0, but 0 * infinity is NaN (an integer
+      // block's infinities and NaN are those of whole channels)
+      if (x.drop) drop_words(y[g], x.drop, 2 * (half + pp) + g, kg);
+    }
   }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) a[c] = u4{y[0][2 * c], y[0][2 * c + 1], y[1][2 * c], y[1][2 * c + 1]};
 }
 
-// With one row tile the scales and zeros of an integer block stay out of its codes' operands, which
-// are 2^k + code as they come from the bits (for four tiles that is more work, not less):
-//   q . k = sum (2^k + code) (q s) + sum z q - sum 2^k (q s), with q s as two fp16 terms and the
-//   constant part from the matrix units too, for any token the same;
-//   sum p v = s (sum p (2^k + code) - 2^k sum p) + z sum p, once a block.
-// Both sums are held in 32 bits, where 2^k <= 1024 costs 2^-14 of a code's step at most.  The rows of
-// q are brought below 1 and s is at most 65504 2 / 3 (two bits), 8734 or 514, so that no q s
-// overflows; those of eight bits are raised by 2^6, so that the second term of one is lost only
-// where 2^-12 of the code's span is less than a step of fp16's smallest numbers.
-constexpr float kRaise = 64.f;
+// q s of a block in two terms, and what its scores start from (eight bits: that times 2^6, and what
+// they end with).
 template <int LEVEL>
 __device__ __forceinline__ void few_fold(u4 (&hi)[4], u4 (&lo)[4], f4 &start, f4 &zero, uint32_t buf, uint32_t lds,
                                          int lane) {
@@ -984,8 +908,8 @@ __device__ __forceinline__ void few_fold(u4 (&hi)[4], u4 (&lo)[4], f4 &start, f4
 // Infinities and NaN among an exact half block's values where some row does not see all of it:
 // out of the product, and noted for the rows that see them (two bits an output, as in
 // ta::find_odd).  The copied values are made clean in place.
-template <int CT>
-__device__ __forceinline__ void few_odd(u4 (&odd)[CT], const uint64_t (&vis)[CT], uint32_t buf, int half, int lane) {
+// vis: the row's visible tokens of the half.
+__device__ __forceinline__ void few_odd(u4 &odd, uint32_t vis, uint32_t buf, int lane) {
   const int kg = lane >> 4;
   float zero = 0.f;
 #pragma unroll 1
@@ -1005,9 +929,7 @@ __device__ __forceinline__ void few_odd(u4 (&odd)[CT], const uint64_t (&vis)[CT]
       for (int i = 0; i < 4; ++i) {
         const uint32_t h = lds_u16(at + (c >> 1) * 1024 + (c & 1) * 8 + i * 16);
         const uint32_t e = h & 0x7FFFu, b = e < T16::kInf ? 0u : e > T16::kInf ? 3u : h == e ? 1u : 2u;
-#pragma unroll
-        for (int t = 0; t < CT; ++t)
-          odd[t][c >> 1] |= (vis[t] >> (32 * half + tok) & 1 ? b : 0u) << (8 * (c & 1) + 2 * i);
+        odd[c >> 1] |= (vis >> tok & 1 ? b : 0u) << (8 * (c & 1) + 2 * i);
       }
   }
 #pragma unroll 1
@@ -1019,294 +941,238 @@ __device__ __forceinline__ void few_odd(u4 (&odd)[CT], const uint64_t (&vis)[CT]
   }
 }
 
-#define GKV_LEVELS(level, f, raw, ...)                               \
-  do {                                                                \
-    if (level == GKV_INT4) f<GKV_INT4, raw>(__VA_ARGS__);             \
-    else if (level == GKV_INT2) f<GKV_INT2, raw>(__VA_ARGS__);        \
-    else if (level == GKV_INT8) f<GKV_INT8, raw>(__VA_ARGS__);        \
-    else if (level == GKV_EXACT) f<GKV_EXACT, raw>(__VA_ARGS__);      \
-    else if (level == GKV_CENTROID) f<GKV_CENTROID, raw>(__VA_ARGS__); \
-    else f<GKV_MEAN, raw>(__VA_ARGS__);                               \
+#define GKV_LEVELS(level, f, ...)                                \
+  do {                                                           \
+    if (level == GKV_INT4) f<GKV_INT4>(__VA_ARGS__);             \
+    else if (level == GKV_INT2) f<GKV_INT2>(__VA_ARGS__);        \
+    else if (level == GKV_INT8) f<GKV_INT8>(__VA_ARGS__);        \
+    else if (level == GKV_EXACT) f<GKV_EXACT>(__VA_ARGS__);      \
+    else if (level == GKV_CENTROID) f<GKV_CENTROID>(__VA_ARGS__); \
+    else f<GKV_MEAN>(__VA_ARGS__);                               \
   } while (0)
 
-template <int CT>
-__global__ void __launch_bounds__(64 * kFewWaves, CT <= 2 ? 2 : 1) few_kernel(const ChunkParams p) {
-  constexpr int kR = 16 * CT;
-  constexpr bool kFold = CT == 1;
-  // the queries' operands, then each wavefront's two buffers, the rows' largest; in the end the
-  // wavefronts' states
-  constexpr int kQ = CT * 4096;
-  __shared__ __align__(16) uint8_t sh[kQ + kFewWaves * 2 * kFewBuf + (kFold ? kFewWaves * 64 : 0)];
-  static_assert((8 * 4 + 2) * CT * 256 * 2 <= sizeof(sh), "two wavefronts' states");
+__global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParams p) {
+  // the queries' operands, then each wavefront's keys and values, the rows' largest; in the end
+  // two wavefronts' states
+  constexpr int kQ = 4096, kTops = kQ + kFewWaves * 2 * kFewBuf, kState = 8 * 1024 + 512;
+  __shared__ __align__(16) uint8_t sh[kTops + kFewWaves * 64];
+  static_assert(2 * kState <= sizeof(sh), "two wavefronts' states");
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)sh;
-  const Job j = job_of(p, kR);
+  const Job j = job_of(p, kFewRows);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int kg = lane >> 4, m = lane & 15;
-  auto token = [&](int t) { return min(16 * t + m, j.rows - 1) / p.G; };  // rows past the last are copies
+  const int row = j.tile * kFewRows + m, rc = min(row, j.rows - 1);  // rows past the last are copies
+  const int tok = rc / p.G, g = rc - tok * p.G;
   const int nvis = j.nblk + (p.nres + P - 1) / P;
   const int split = p.split[j.s];
   // every workgroup takes blocks from the whole context in turn, so that each gets as many of
   // each level (in runs of blocks the ones with the exact blocks took a third longer)
-  const int v1 = nvis, stride = split * kFewWaves;
+  const int stride = split * kFewWaves;
   const uint32_t kbuf = lds + kQ + wave * 2 * kFewBuf, vbuf = kbuf + kFewBuf;
   int at = j.part * kFewWaves + wave, half = 0, nth = 0;
   Visits batch = {};
   Visit x, next;
-  if (at < v1) {
-    batch.read(p, j, at, stride, v1, lane);
+  if (at < nvis) {
+    batch.read(p, j, at, stride, nvis, lane);
     x = batch.at(0);
     few_copy(x.k, x.level, 0, kbuf, lane);
   }
   float sl2 = p.sl2;
-#pragma unroll
-  for (int t = 0; t < CT; ++t) {  // a wavefront copies channels 32 wave .. + 31
-    const int rc = min(16 * t + m, j.rows - 1), tok = rc / p.G, g = rc - tok * p.G;
+  {  // a wavefront copies channels 32 wave .. + 31 of the queries, times the power of two that brings
+     // the row's largest below 1
     u4 q = *(const u4 *)(p.q + (j.row0 + tok) * p.qs + (int64_t)(j.h * p.G + g) * D + 8 * kg + 32 * wave);
-    if constexpr (kFold) {
-      // times the power of two that brings the row's largest below 1: a scale is at most
-      // 65504 2 / 3, so that their product is finite
-      uint32_t top = 0;
+    uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, max(q[i] & 0x7FFFu, q[i] >> 16 & 0x7FFFu));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-      const uint32_t tops = lds + kQ + kFewWaves * 2 * kFewBuf;
-      if (lane < 16) *(LdsW1)(uintptr_t)(tops + (wave * 16 + m) * 4) = top;
-      __syncthreads();
+    for (int i = 0; i < 4; ++i) top = max(top, max(q[i] & 0x7FFFu, q[i] >> 16 & 0x7FFFu));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    if (lane < 16) *(LdsW1)(uintptr_t)(lds + kTops + (wave * 16 + m) * 4) = top;
+    __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kFewWaves; ++i) top = max(top, *(LdsW1)(uintptr_t)(tops + (i * 16 + m) * 4));
-      const int k = top == 0 || top >= T16::kInf ? 0 : 14 - (int)(top >> 10);
-      const uint32_t f = (k >= -14 ? (15 + k) << 10 : 0x400 >> (-14 - k)) * 0x10001u;
+    for (int i = 0; i < kFewWaves; ++i) top = max(top, *(LdsW1)(uintptr_t)(lds + kTops + (i * 16 + m) * 4));
+    const int k = top == 0 || top >= T16::kInf ? 0 : 14 - (int)(top >> 10);
+    const uint32_t f = (k >= -14 ? (15 + k) << 10 : 0x400 >> (-14 - k)) * 0x10001u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = __builtin_bit_cast(uint32_t, halves(q[i]) * halves(f));
-      sl2 = ldexpf(sl2, -k);
-    }
-    *(LdsW4)(uintptr_t)(lds + (t * 4 + wave) * 1024 + lane * 16) = q;
+    for (int i = 0; i < 4; ++i) q[i] = __builtin_bit_cast(uint32_t, halves(q[i]) * halves(f));
+    sl2 = ldexpf(sl2, -k);
+    *(LdsW4)(uintptr_t)(lds + wave * 1024 + lane * 16) = q;
   }
   const Exponents e;
-  FewRows<CT> r;
-  u4 odd[CT];
+  FewRows r;
+  u4 odd = {0, 0, 0, 0};
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-#pragma unroll
-    for (int c = 0; c < 8; ++c) r.o[c][t] = f4{0.f, 0.f, 0.f, 0.f};
-    r.m[t] = r.l[t] = 0.f;
-    r.raise[t] = -__builtin_inff();
-    odd[t] = u4{0, 0, 0, 0};
-  }
+  for (int c = 0; c < 8; ++c) r.o[c] = f4{0.f, 0.f, 0.f, 0.f};
+  r.m = r.l = 0.f;
+  r.raise = -__builtin_inff();
   __syncthreads();
-  while (at < v1) {
+  while (at < nvis) {
     const bool again = x.level == GKV_EXACT && half == 0;  // the block's other half is next
     const int after = again ? at : at + stride;
+    const bool more = after < nvis;
     next = x;
-    if (!again && after < v1) {
+    if (!again && more) {
       nth = (nth + 1) & 63;
-      if (nth == 0) batch.read(p, j, after, stride, v1, lane);
+      if (nth == 0) batch.read(p, j, after, stride, nvis, lane);
       next = batch.at(nth);
     }
     const bool whole = whole_at(p, j, at, j.pos0);
     few_copy(x.v, x.level, half, vbuf, lane);
     few_wait(x.level);
+    const bool codes = is_codes(x.level);
     const bool two = x.level != GKV_EXACT && x.level != GKV_MEAN;  // pairs of pages
-    f4 s[4][CT];
-    const bool codes = x.level == GKV_INT8 || x.level == GKV_INT4 || x.level == GKV_INT2;
-    u4 hi[4], lo[4];
-    f4 start = {0.f, 0.f, 0.f, 0.f}, zero;
-    if constexpr (kFold) {
+    f4 s[4], start = {0.f, 0.f, 0.f, 0.f}, zero;
+    {
+      u4 hi[4], lo[4];
       if (x.level == GKV_INT4) few_fold<GKV_INT4>(hi, lo, start, zero, kbuf, lds, lane);
       else if (x.level == GKV_INT2) few_fold<GKV_INT2>(hi, lo, start, zero, kbuf, lds, lane);
       else if (x.level == GKV_INT8) few_fold<GKV_INT8>(hi, lo, start, zero, kbuf, lds, lane);
       else
 #pragma unroll
         for (int d = 0; d < 4; ++d) hi[d] = ta::lds_u4(lds + d * 1024 + lane * 16);
-    }
 #pragma unroll
-    for (int pp = 0; pp < 2; ++pp) {
-      if (pp == 0 || two) {
-        u4 a[8];
-        GKV_LEVELS(x.level, few_keys, kFold, a, kbuf, pp, lane, e);
+      for (int pp = 0; pp < 2; ++pp)
+        if (pp == 0 || two) {
+          u4 a[8];
+          GKV_LEVELS(x.level, few_keys, a, kbuf, pp, lane, e);
+          s[2 * pp] = s[2 * pp + 1] = start;
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          s[2 * pp][t] = s[2 * pp + 1][t] = start;
+          for (int d = 0; d < 4; ++d)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const u4 q = kFold ? hi[d] : ta::lds_u4(lds + (t * 4 + d) * 1024 + lane * 16);
-#pragma unroll
-            for (int g = 0; g < 2; ++g) s[2 * pp + g][t] = mfma16(a[4 * g + d], q, s[2 * pp + g][t]);
-          }
-          if (kFold && codes)
+            for (int h = 0; h < 2; ++h) s[2 * pp + h] = mfma16(a[4 * h + d], hi[d], s[2 * pp + h]);
+          if (codes)
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-              for (int g = 0; g < 2; ++g) s[2 * pp + g][t] = mfma16(a[4 * g + d], lo[d], s[2 * pp + g][t]);
+              for (int h = 0; h < 2; ++h) s[2 * pp + h] = mfma16(a[4 * h + d], lo[d], s[2 * pp + h]);
         }
-      }
-      if (!kFold) asm volatile("" ::: "memory");  // the queries' operands are read again (kept, they spill)
     }
-    if (kFold && x.level == GKV_INT8) {
+    few_read();
+    if (more) few_copy(next.k, next.level, again ? 1 : 0, kbuf, lane);
+    if (x.level == GKV_INT8) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
+      for (int h = 0; h < 4; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[g][0][i] = __builtin_fmaf(s[g][0][i], 1.f / kRaise, zero[i]);
+        for (int i = 0; i < 4; ++i) s[h][i] = __builtin_fmaf(s[h][i], 1.f / kRaise, zero[i]);
     }
-    if (!two) {
-#pragma unroll
-      for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[2][t][i] = s[3][t][i] = -__builtin_inff();
-    }
+    const float no = -__builtin_inff();
+    if (!two) s[2] = s[3] = f4{no, no, no, no};
     if (x.level == GKV_MEAN) {
       // one key stands for all the block's tokens: its weight times their number, in the first
       // group's first place alone
       const int n = P - __popcll(x.drop);
-      const float more = __builtin_amdgcn_logf((float)n) / sl2, no = -__builtin_inff();
-#pragma unroll
-      for (int t = 0; t < CT; ++t) {
-        s[0][t][0] = lane < 16 && n ? s[0][t][0] + more : no;
-        s[0][t][1] = s[0][t][2] = s[0][t][3] = no;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[1][t][i] = no;
-      }
+      const float plus = __builtin_amdgcn_logf((float)n) / sl2;
+      s[0] = f4{lane < 16 && n ? s[0][0] + plus : no, no, no, no};
+      s[1] = f4{no, no, no, no};
     }
-    few_read();
-    if (after < v1) few_copy(next.k, next.level, again ? 1 : 0, kbuf, lane);
-    uint64_t vis[CT];
+    uint32_t seen = 0;
     if (!whole || (x.drop && x.level != GKV_MEAN)) {
+      const uint64_t vis = (whole ? ~x.drop : seen_by(p, j, at, x.drop, j.pos0 + tok)) >> (32 * half);
+      seen = (uint32_t)vis;
+      const uint64_t w = vis >> (4 * kg);
 #pragma unroll
-      for (int t = 0; t < CT; ++t) {
-        vis[t] = whole ? ~x.drop : seen_by(p, j, at, x.drop, j.pos0 + token(t));
-        const uint64_t w = vis[t] >> (32 * half + 4 * kg);
+      for (int h = 0; h < 4; ++h)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[g][t][i] = w >> (16 * g + i) & 1 ? s[g][t][i] : -__builtin_inff();
-      }
+        for (int i = 0; i < 4; ++i) s[h][i] = w >> (16 * h + i) & 1 ? s[h][i] : no;
     }
-    uint32_t w[CT][8];
-    few_weights<CT>(w, r, s, sl2);
-    few_wait(after < v1 ? next.level : -1);
-    if (!whole) few_odd<CT>(odd, vis, vbuf, half, lane);  // an exact block (the host sees to it)
-    const bool scaled = kFold && codes && !p.vtok;
-    f4 acc[kFold ? 8 : 1];
+    uint32_t w[8];
+    few_weights(w, r, s, sl2);
     float sum = 0.f;  // of the step's weights
-    if constexpr (kFold) {
-      if (scaled) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = T16::add2(w[0][i], sum);
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-      }
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const uint32_t off = x.level == GKV_INT8   ? raw_offset<8>(2 * c)
-                             : x.level == GKV_INT4 ? raw_offset<4>(2 * c)
-                                                   : raw_offset<2>(2 * c);
-        const float z = scaled ? -(float)halves(off)[0] * sum : 0.f;
-        acc[c] = f4{z, z, z, z};
-      }
+    for (int i = 0; i < 8; ++i) sum = T16::add2(w[i], sum);
+    r.l += sum;
+    const bool scaled = codes && !p.vtok;
+    f4 acc[8];
+    if (scaled) {
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
     }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t off = x.level == GKV_INT8   ? raw_offset<8>(2 * c)
+                           : x.level == GKV_INT4 ? raw_offset<4>(2 * c)
+                                                 : raw_offset<2>(2 * c);
+      const float z = scaled ? -(float)halves(off)[0] * sum : 0.f;
+      acc[c] = f4{z, z, z, z};
+    }
+    few_wait(more ? next.level : -1);
+    if (!whole) few_odd(odd, seen, vbuf, lane);  // an exact block (the host sees to it)
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp)
       if (pp == 0 || two) {
         u4 a[8];
-        GKV_LEVELS(x.level, few_values, kFold, a, x, half, vbuf, pp, p.vtok, lane, e);
+        GKV_LEVELS(x.level, few_values, a, x, half, vbuf, pp, p.vtok, lane, e);
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int t = 0; t < CT; ++t) {
-            const u4 b = {w[t][4 * pp], w[t][4 * pp + 1], w[t][4 * pp + 2], w[t][4 * pp + 3]};
-            if constexpr (kFold) acc[c] = mfma16(a[c], b, acc[c]);
-            else r.o[c][t] = mfma16(a[c], b, r.o[c][t]);
-          }
+          acc[c] = mfma16(a[c], u4{w[4 * pp], w[4 * pp + 1], w[4 * pp + 2], w[4 * pp + 3]}, acc[c]);
       }
-    if constexpr (kFold) {
-      // channels 16 c + 4 kg .. + 3 lie side by side in the header's lane order
-      if (scaled) {
+    if (scaled) {  // channels 16 c + 4 kg .. + 3 lie side by side in the header's lane order
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const u4 sc = ta::lds_u4(vbuf + kg * 64 + h * 16), z = ta::lds_u4(vbuf + 256 + kg * 64 + h * 16);
+      for (int h = 0; h < 4; ++h) {
+        const u4 sc = ta::lds_u4(vbuf + kg * 64 + h * 16), z = ta::lds_u4(vbuf + 256 + kg * 64 + h * 16);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            f4 &o = r.o[2 * h + (i >> 2)][0];
-            const float y = __builtin_fmaf((float)halves(sc[i >> 1])[i & 1], acc[2 * h + (i >> 2)][i & 3], o[i & 3]);
-            o[i & 3] = __builtin_fmaf((float)halves(z[i >> 1])[i & 1], sum, y);
-          }
+        for (int i = 0; i < 8; ++i) {
+          f4 &o = r.o[2 * h + (i >> 2)];
+          const float y = __builtin_fmaf((float)halves(sc[i >> 1])[i & 1], acc[2 * h + (i >> 2)][i & 3], o[i & 3]);
+          o[i & 3] = __builtin_fmaf((float)halves(z[i >> 1])[i & 1], sum, y);
         }
-      } else {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) r.o[c][0] += acc[c];
       }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) r.o[c] += acc[c];
     }
     few_read();
     x = next;
     half = again;
     at = after;
   }
+  r.l += __shfl_xor(r.l, 16);
+  r.l += __shfl_xor(r.l, 32);
+  if (__any(odd[0] | odd[1] | odd[2] | odd[3]))  // the values that stayed out of the products
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const uint32_t b = odd[i >> 3] >> (8 * (i >> 2 & 1) + 2 * (i & 3)) & 3u;  // 0, infinity, -infinity, NaN
+      const uint32_t v = (b & 1u ? 0x7F800000u : b ? 0xFF800000u : 0u) | (b == 3 ? 0x400000u : 0u);
+      r.o[i >> 2][i & 3] += __builtin_bit_cast(float, v);
+    }
   // the wavefronts' states, joined two and two in LDS, each value in the lane that holds its like
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    r.l[t] += __shfl_xor(r.l[t], 16);
-    r.l[t] += __shfl_xor(r.l[t], 32);
-    if (__any(odd[t][0] | odd[t][1] | odd[t][2] | odd[t][3]))  // the values that stayed out of the products
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const uint32_t b = odd[t][i >> 3] >> (8 * (i >> 2 & 1) + 2 * (i & 3)) & 3u;  // 0, infinity, -infinity, NaN
-        const uint32_t v = (b & 1u ? 0x7F800000u : b ? 0xFF800000u : 0u) | (b == 3 ? 0x400000u : 0u);
-        r.o[i >> 2][t][i & 3] += __builtin_bit_cast(float, v);
-      }
-  }
-#pragma unroll
-  for (int n = 2; n >= 1; n >>= 1) {
+  for (int n = kFewWaves / 2; n >= 1; n >>= 1) {
     __syncthreads();
-    const uint32_t mine = lds + (wave & (n - 1)) * ((8 * 4 + 2) * CT * 256) + lane * 16;
-    if (wave >= n && wave < 2 * n)
+    const uint32_t mine = lds + (wave & (n - 1)) * kState + lane * 16, ends = mine - lane * 8 + 8192;
+    if (wave >= n && wave < 2 * n) {
 #pragma unroll
-      for (int t = 0; t < CT; ++t) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) *(LdsF4)(uintptr_t)(mine + (t * 8 + c) * 1024) = r.o[c][t];
-        *(LdsF2)(uintptr_t)(mine - lane * 8 + CT * 8192 + t * 512) = f2{r.m[t], r.l[t]};
-      }
-    __syncthreads();
-    if (wave < n)
-#pragma unroll
-      for (int t = 0; t < CT; ++t) {
-        const f2 ml = *(LdsF2)(uintptr_t)(mine - lane * 8 + CT * 8192 + t * 512);
-        // a state that has seen nothing has no maximum
-        const float top = r.l[t] == 0.f ? ml[0] : ml[1] == 0.f ? r.m[t] : fmaxf(r.m[t], ml[0]);
-        const float a = r.l[t] == 0.f ? 0.f : __builtin_amdgcn_exp2f(r.m[t] - top);
-        const float b = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
-        r.m[t] = top;
-        r.l[t] = r.l[t] * a + ml[1] * b;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const f4 o = *(LdsF4)(uintptr_t)(mine + (t * 8 + c) * 1024);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) r.o[c][t][i] = r.o[c][t][i] * a + o[i] * b;
-        }
-      }
-  }
-  if (wave) return;
-#pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    const int i = 16 * t + m;
-    if (i >= j.rows) continue;
-    if (split == 1) {
-      const float inv = r.l[t] > 0.f ? 1.f / r.l[t] : r.l[t];
-      const int tok = i / p.G, g = i - tok * p.G;
-      uint16_t *op = p.out + (j.row0 + tok) * p.os + (int64_t)(j.h * p.G + g) * D + 4 * kg;
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        *(u2 *)(op + 16 * c) = u2{T16::pack(r.o[c][t][0] * inv, r.o[c][t][1] * inv),
-                                  T16::pack(r.o[c][t][2] * inv, r.o[c][t][3] * inv)};
-    } else {
-      float *part = p.part + (part_row(p, j, kR) + i) * kPart;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        *(float2 *)(part + 16 * c + 4 * kg) = make_float2(r.o[c][t][0], r.o[c][t][1]);
-        *(float2 *)(part + 16 * c + 4 * kg + 2) = make_float2(r.o[c][t][2], r.o[c][t][3]);
-      }
-      if (kg == 0) *(float2 *)(part + D) = make_float2(r.m[t], r.l[t]);
+      for (int c = 0; c < 8; ++c) *(LdsF4)(uintptr_t)(mine + c * 1024) = r.o[c];
+      *(LdsF2)(uintptr_t)ends = f2{r.m, r.l};
     }
+    __syncthreads();
+    if (wave < n) {
+      const f2 ml = *(LdsF2)(uintptr_t)ends;
+      // a state that has seen nothing has no maximum
+      const float top = r.l == 0.f ? ml[0] : ml[1] == 0.f ? r.m : fmaxf(r.m, ml[0]);
+      const float a = r.l == 0.f ? 0.f : __builtin_amdgcn_exp2f(r.m - top);
+      const float b = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
+      r.m = top;
+      r.l = r.l * a + ml[1] * b;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) r.o[c] = r.o[c] * a + *(LdsF4)(uintptr_t)(mine + c * 1024) * b;
+    }
+  }
+  if (wave || row >= j.rows) return;
+  if (split == 1) {
+    const float inv = r.l > 0.f ? 1.f / r.l : r.l;
+    uint16_t *op = p.out + (j.row0 + tok) * p.os + (int64_t)(j.h * p.G + g) * D + 4 * kg;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      *(u2 *)(op + 16 * c) = u2{T16::pack(r.o[c][0] * inv, r.o[c][1] * inv),
+                                T16::pack(r.o[c][2] * inv, r.o[c][3] * inv)};
+  } else {
+    float *part = p.part + (part_row(p, j, kFewRows) + m) * kPart;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      *(float2 *)(part + 16 * c + 4 * kg) = make_float2(r.o[c][0], r.o[c][1]);
+      *(float2 *)(part + 16 * c + 4 * kg + 2) = make_float2(r.o[c][2], r.o[c][3]);
+    }
+    if (kg == 0) *(float2 *)(part + D) = make_float2(r.m, r.l);
   }
 }
 #undef GKV_LEVELS
@@ -1361,10 +1227,12 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, i
 }
 
 // ---------------------------------------------------------------- host
-// Rows of a (sequence, KV head) up to which its blocks are read by few_kernel, decoded for every
-// wavefront's rows anew; beyond, the cache is decoded to tiles first, which costs its
-// bytes written and read again (0.26 ns a token of a KV head, as much as 512 rows' products).
-constexpr int kFewMost = 64;
+// Rows of a (sequence, KV head) up to which its blocks are read by few_kernel, decoded for every 16 rows
+// anew; beyond, the cache is decoded to tiles first, which costs its bytes written and read
+// again, and row tiles are of 256.  4 KV heads, few and many rows' form in us: 8 x 32k tokens 14
+// rows 52 and 307, 63 rows 148 and 297, 126 rows 275 and 305; 1 x 64k 39 and 84, 49 and 86, 80 and
+// 89; 16 x 2000 25 and 51, 35 and 53, 45 and 57.
+constexpr int kFewMost = 128;
 constexpr int kLeastVisits = 4;  // blocks that a workgroup takes at least
 constexpr int64_t kCus = 256;
 
@@ -1437,7 +1305,7 @@ struct Plan {
 gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
   const int G = c->Hq / c->Hkv;
   pl.few.p.nseq = pl.many.p.nseq = 0;
-  int64_t rows = 0, most = 0;
+  int64_t rows = 0;
   for (int b = 0; b < c->B; ++b) {
     const int64_t T = seq_tokens(c, b), n = n_new[b];
     if (n < 0) return GKV_E_SHAPE;
@@ -1456,11 +1324,10 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
     p.n[i] = (int32_t)n;
     p.row0[i] = (int32_t)rows;
     rows += n;
-    if (few && n * G > most) most = n * G;
   }
-  pl.few.rows_tile = (int)((most + 15) / 16 * 16);
+  pl.few.rows_tile = kFewRows;
   pl.many.rows_tile = 256;
-  gkv_status st = plan_part(pl.few, c, pl.few.rows_tile <= 32 ? 2 * kCus : kCus);
+  gkv_status st = plan_part(pl.few, c, 2 * kCus);
   if (!st) st = plan_part(pl.many, c, kCus);
   if (st) return st;
   auto align = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
@@ -1469,16 +1336,6 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
   pl.list = align(pl.whole + (int64_t)pl.many.p.nseq * c->Hkv * 4);
   pl.bytes = pl.list + pl.many.tiles * kListTile;
   return GKV_OK;
-}
-
-void launch_few(const Part &t, const dim3 grid, hipStream_t s) {
-  const dim3 blk(64 * kFewWaves);
-  switch (t.rows_tile) {
-    case 16: hipLaunchKernelGGL((few_kernel<1>), grid, blk, 0, s, t.p); break;
-    case 32: hipLaunchKernelGGL((few_kernel<2>), grid, blk, 0, s, t.p); break;
-    case 48: hipLaunchKernelGGL((few_kernel<3>), grid, blk, 0, s, t.p); break;
-    default: hipLaunchKernelGGL((few_kernel<4>), grid, blk, 0, s, t.p); break;
-  }
 }
 
 }  // namespace
@@ -1538,7 +1395,7 @@ extern "C" gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const 
     p.list = (uint8_t *)ws + pl.list;
     const dim3 grid((unsigned)(t->wgs * c->Hkv));
     if (t == &pl.few) {
-      launch_few(*t, grid, s);
+      hipLaunchKernelGGL(few_kernel, grid, dim3(64 * kFewWaves), 0, s, p);
     } else {
       int most = 0;
       for (int i = 0; i < p.nseq; ++i) most = std::max(most, list_tiles(p.T[i], c->nres));

@@ -283,11 +283,10 @@ def test_long_contexts_are_split(gpu, prof, T, n):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("Hq,n", [(1, 15), (1, 16), (1, 17), (1, 31), (1, 32), (1, 33), (1, 48), (1, 49), (1, 64), (1, 65),
-                                  (4, 4), (4, 5), (7, 2), (7, 3), (5, 9), (5, 13), (16, 4), (16, 5)])
+                                  (4, 4), (4, 5), (7, 2), (7, 3), (5, 9), (5, 13), (16, 4), (16, 5), (16, 8), (16, 9)])
 @pytest.mark.parametrize("vtok,nres", [(False, 0), (True, 70)])
 def test_row_counts(gpu, Hq, n, vtok, nres):
-    """Rows about every bound of a row tile, over all six levels (the newest rows exact: the
-    few-row form; see test_rows_in_demoted_blocks for the other)."""
+    """Rows about every bound of a row tile and of the two forms, over all six levels."""
     T = 64 * 40 + 5
     c = Case(gpu, 73, (T,), (n,), Hq, 1, mixed_levels, vtok=vtok, nres=nres, ragged=False)
     c.check(c.run())
