@@ -383,8 +383,8 @@ __device__ __forceinline__ void dma16(uint32_t voff, const void *base, uint32_t 
 //
 // Intervals, each ended by a barrier: the first wavefronts' key product of tile t is in interval
 // 2 t, the second ones' in 2 t + 1.  Keys t + 1 and values t are copied from the start of
-// interval 2 t on (whose buffers were last read in 2 t - 1) and have arrived at the end of
-// 2 t + 1.
+// interval 2 t on (whose buffers were last read in 2 t - 1; the first ones from the start on) and
+// have arrived at the end of 2 t + 1.
 template <class T, int WAVES, bool kTr, bool kBias, class Src, class Seen, class Load>
 __device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uint32_t lds, int wave, int t0, int t1,
                                        int full, float sl2, const Src &src, const Seen &seen, const Load &load) {
@@ -414,6 +414,7 @@ __device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uin
     if (second) copy(t + 2);
   };
   copy_keys(t0);
+  copy(t0);
   load();
   // the queries have arrived (the loop's copies are in flight when they are used: a wait for
   // their loads there would wait for the copies)
@@ -425,11 +426,7 @@ __device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uin
   if (full > t1 - 1) full = t1 - 1;
   arrived();
   meet();
-  copy(t0);
-  if (second) {
-    arrived();
-    meet();
-  }
+  if (second) meet();
   scores<T, kBias>(s, ln, q, keys(t0), bias(t0));
   after(t0 - 1);
   int t = t0;
