@@ -40,7 +40,7 @@ struct ChunkAppend {
   int64_t npage_cap;
   float *cert;       // or null
   int64_t *seq_len;  // or null
-  int32_t page, Hkv, nblk_cap, nseq;
+  int32_t page, Hkv, nblk_cap;
   int32_t first_launch, nrun;
   SlotRun run[kMaxRuns];
   int64_t T[kMaxSeqs];  // tokens before the call (-1: retired)
@@ -56,7 +56,6 @@ __device__ __forceinline__ int key_half(int tok, int d) {  // half index of an e
 // chunks and by the launch for drafts.
 __global__ void __launch_bounds__(kThreads) append_chunk_kernel(const ChunkAppend p) {
   __shared__ __align__(16) uint16_t kt[P * kRowPad], vt[P * kRowPad];
-  __shared__ double norm[P];
   const int h = blockIdx.y, tid = threadIdx.x;
   // the sequence and block of this workgroup, the sequence's first packed row and first slot
   int64_t row0 = 0;
@@ -142,28 +141,33 @@ __global__ void __launch_bounds__(kThreads) append_chunk_kernel(const ChunkAppen
   }
 
   if (p.cert) {  // an exact block: no error; the value norms, each a channel-ascending sum
-    if (tid < P) {
+    if (tid < P) {  // (one wavefront)
       double s = 0.0;
       if (tid >= lo && tid < hi)
-        for (int d = 0; d < D; ++d) {
-          const double x = (double)__builtin_bit_cast(_Float16, vt[tid * kRowPad + d]);
-          s += x * x;
+#pragma unroll 4
+        for (int d = 0; d < D; d += 8) {
+          const w4 w = *(const w4 *)(vt + tid * kRowPad + d);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const double x = (double)__builtin_bit_cast(_Float16, (uint16_t)(w[i >> 1] >> (16 * (i & 1))));
+            s += x * x;
+          }
         }
-      norm[tid] = s;
-    }
-    __syncthreads();
-    if (tid == 0) {
-      double s = 0.0;
-      for (int t = lo; t < hi; ++t) s = norm[t] > s ? norm[t] : s;
-      const float vn = enc::round_up_f32(__builtin_sqrt(s));
-      float *cb = p.cert + ti * 4;
-      if (open) {
-        cb[0] = 0.f;
-        cb[1] = 0.f;
-        cb[2] = vn;
-        cb[3] = 0.f;
-      } else {
-        cb[2] = vn > cb[2] ? vn : cb[2];
+      for (int k = 1; k < P; k <<= 1) {
+        const double y = __shfl_xor(s, k);
+        s = y > s ? y : s;
+      }
+      if (tid == 0) {
+        const float vn = enc::round_up_f32(__builtin_sqrt(s));
+        float *cb = p.cert + ti * 4;
+        if (open) {
+          cb[0] = 0.f;
+          cb[1] = 0.f;
+          cb[2] = vn;
+          cb[3] = 0.f;
+        } else {
+          cb[2] = vn > cb[2] ? vn : cb[2];
+        }
       }
     }
   }
@@ -251,16 +255,24 @@ static gkv_status append_chunk(gkv_cache *c, const uint16_t *k_new, const uint16
     if (s % 8) return GKV_E_ARG;
     if (s > GKV_MAX_ROW_STRIDE) return GKV_E_UNSUPPORTED;
   }
-  std::vector<int64_t> slots;
-  slots.reserve(2 * (size_t)n_open);
-  for (int i = 0; i < n_open; ++i)
-    for (const int64_t off : {koff[i], voff[i]}) {
-      if (off < 0 || off % 16 || off + kExactBytes > c->arena_bytes) return GKV_E_ARG;
-      slots.push_back(off);
-    }
-  std::sort(slots.begin(), slots.end());
-  for (size_t i = 1; i < slots.size(); ++i)
-    if (slots[i] - slots[i - 1] < kExactBytes) return GKV_E_ARG;  // two blocks in one place
+  // every slot in the arena, no two in one place: seen at once where they stand in order, as an
+  // unfragmented pool hands them out
+  bool up = true, down = true;
+  int64_t last = 0;
+  for (int i = 0; i < 2 * n_open; ++i) {
+    const int64_t off = i & 1 ? voff[i >> 1] : koff[i >> 1];
+    if (off < 0 || off % 16 || off + kExactBytes > c->arena_bytes) return GKV_E_ARG;
+    up &= !i || off - last >= kExactBytes;
+    down &= !i || last - off >= kExactBytes;
+    last = off;
+  }
+  if (!up && !down) {
+    std::vector<int64_t> slots(koff, koff + n_open);
+    slots.insert(slots.end(), voff, voff + n_open);
+    std::sort(slots.begin(), slots.end());
+    for (size_t i = 1; i < slots.size(); ++i)
+      if (slots[i] - slots[i - 1] < kExactBytes) return GKV_E_ARG;
+  }
   p.k_new = k_new;
   p.v_new = v_new;
   p.ks = k_stride;
@@ -276,7 +288,6 @@ static gkv_status append_chunk(gkv_cache *c, const uint16_t *k_new, const uint16
   p.page = c->page ? c->page : P;
   p.Hkv = c->Hkv;
   p.nblk_cap = c->nblk_cap;
-  p.nseq = c->B;
   p.first_launch = 1;
   int i = 0;
   do {  // one launch, more if the slots make more runs than one takes
