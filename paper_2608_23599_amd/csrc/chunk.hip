@@ -827,27 +827,32 @@ template <int LEVEL>
 __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half, uint32_t buf, int pp, bool vtok,
                                            int lane, const Exponents &e) {
   const int kg = lane >> 4, m = lane & 15;
-  uint32_t y[2][16];
+  // word q of page g's chunk (tokens 4 kg + 2 (q & 1) and the next, channel 16 (q >> 1) + m) is
+  // a[q >> 1][2 g + (q & 1)]
   if constexpr (LEVEL == GKV_MEAN) {  // the one key's place alone
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
       const uint32_t v = lds_u16(buf + 2 * (16 * c + m));
       a[c] = u4{lane < 16 ? v : 0, 0, 0, 0};
     }
-    return;
   } else if constexpr (is_codes(LEVEL)) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       Raw w;
       few_codes<LEVEL>(w, buf, 2 * pp + g, lane);
 #pragma unroll
-      for (int q = 0; q < 16; ++q) y[g][q] = raw_pair<LEVEL>(w.w, q, e);
-      if (vtok) {  // scales of tokens: into the values here
+      for (int q = 0; q < 16; ++q) a[q >> 1][2 * g + (q & 1)] = raw_pair<LEVEL>(w.w, q, e);
+    }
+    if (vtok) {  // scales of tokens: into the values here
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
         const uint32_t at = buf + (16 * (2 * pp + g) + 4 * kg) * 2;
         const u2 s = *(LdsW2)(uintptr_t)at, z = *(LdsW2)(uintptr_t)(at + 128);
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
-          y[g][q] = decoded(halves(y[g][q]) - halves(raw_offset<LEVEL>(q)), s[q & 1], z[q & 1]);
+        for (int q = 0; q < 16; ++q) {
+          const uint32_t y = a[q >> 1][2 * g + (q & 1)];
+          a[q >> 1][2 * g + (q & 1)] = decoded(halves(y) - halves(raw_offset<LEVEL>(q)), s[q & 1], z[q & 1]);
+        }
       }
     }
   } else {
@@ -857,23 +862,24 @@ __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half,
       for (int i = 0; i < 4; ++i) cent[i] = ta::lds_u4(buf + m * 64 + 16 * i);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
+      uint32_t y[16];
       if constexpr (LEVEL == GKV_CENTROID) {
-        centroid_words(y[g], cent, *(LdsW1)(uintptr_t)(buf + KC * D * 2 + 4 * (2 * pp + g)) >> (8 * kg));
+        centroid_words(y, cent, *(LdsW1)(uintptr_t)(buf + KC * D * 2 + 4 * (2 * pp + g)) >> (8 * kg));
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const u4 b = ta::lds_u4(buf + g * 4096 + j * 1024 + lane * 16);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[g][4 * j + i] = b[i];
+          for (int i = 0; i < 4; ++i) y[4 * j + i] = b[i];
         }
       }
       // a token that is read elsewhere has weight 0, but 0 * infinity is NaN (an integer
       // block's infinities and NaN are those of whole channels)
-      if (x.drop) drop_words(y[g], x.drop, 2 * (half + pp) + g, kg);
+      if (x.drop) drop_words(y, x.drop, 2 * (half + pp) + g, kg);
+#pragma unroll
+      for (int q = 0; q < 16; ++q) a[q >> 1][2 * g + (q & 1)] = y[q];
     }
   }
-#pragma unroll
-  for (int c = 0; c < 8; ++c) a[c] = u4{y[0][2 * c], y[0][2 * c + 1], y[1][2 * c], y[1][2 * c + 1]};
 }
 
 // q s of a block in two terms, and what its scores start from (eight bits: that times 2^6, and what
@@ -1087,12 +1093,12 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParam
       sum += __shfl_xor(sum, 32);
     }
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const uint32_t off = x.level == GKV_INT8   ? raw_offset<8>(2 * c)
-                           : x.level == GKV_INT4 ? raw_offset<4>(2 * c)
-                                                 : raw_offset<2>(2 * c);
+    for (int c = 0; c < 8; ++c) {  // (repeats after four)
+      const uint32_t off = x.level == GKV_INT8   ? raw_offset<8>(2 * (c & 3))
+                           : x.level == GKV_INT4 ? raw_offset<4>(2 * (c & 3))
+                                                 : raw_offset<2>(2 * (c & 3));
       const float z = scaled ? -(float)halves(off)[0] * sum : 0.f;
-      acc[c] = f4{z, z, z, z};
+      acc[c] = c < 4 ? f4{z, z, z, z} : acc[c & 3];
     }
     few_wait(more ? next.level : -1);
     if (!whole) few_odd(odd, seen, vbuf, lane);  // an exact block (the host sees to it)
