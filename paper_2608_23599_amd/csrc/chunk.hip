@@ -328,10 +328,10 @@ struct Job {
   int64_t u, row0;
 };
 
-__device__ __forceinline__ Job job_of(const ChunkParams &p, int rows_tile) {
+__device__ __forceinline__ Job job_of(const ChunkParams &p, int rows_tile, int h, int w) {
   Job j;
-  j.h = blockIdx.x % p.Hkv;
-  int w = blockIdx.x / p.Hkv, lo = 0, hi = p.nseq;
+  j.h = h;
+  int lo = 0, hi = p.nseq;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (p.wg0[mid] <= w) lo = mid;
@@ -595,7 +595,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams 
   extern __shared__ __align__(16) unsigned char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
   constexpr int kTileRows = 32 * WAVES;
-  const Job j = job_of(p, kTileRows);
+  const Job j = job_of(p, kTileRows, blockIdx.x % p.Hkv, blockIdx.x / p.Hkv);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   ta::Lane ln;
   ln.init<false>();
@@ -964,7 +964,11 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParam
   __shared__ __align__(16) uint8_t sh[kTops + kFewWaves * 64];
   static_assert(2 * kState <= sizeof(sh), "two wavefronts' states");
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)sh;
-  const Job j = job_of(p, kFewRows);
+  // the row tiles of a share of the context read the same blocks: side by side on one XCD (workgroups
+  // go round the eight of them), from whose L2 all but the first take them
+  const int x8 = blockIdx.x & 7, each = gridDim.x >> 3, wgs = p.wg0[p.nseq];
+  const int place = x8 * each + min(x8, (int)(gridDim.x & 7)) + (int)(blockIdx.x >> 3);
+  const Job j = job_of(p, kFewRows, place / wgs, place % wgs);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int kg = lane >> 4, m = lane & 15;
   const int row = j.tile * kFewRows + m, rc = min(row, j.rows - 1);  // rows past the last are copies
