@@ -454,10 +454,12 @@ gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, 
  *   out[i][g][:] = sum_{j <= t} softmax_j(q_ig . k_j / sqrt(128)) v_j.
  * q, out: packed rows of [Hq][128] fp16, sequence after sequence, q_stride / out_stride
  * elements from token to token (rules as for gkv_prompt_attn); out must not overlap q.
- * Graded entries are decoded to fp16 (one rounding of code * scale + zero) and
- * probabilities enter the value product in fp16; logits, maxima and sums are fp32.  A token
- * that a row does not see has no effect on it, whatever it holds.  n_new_host[b] is at most
- * the sequence's length (GKV_E_SHAPE) and 0 for a retired one (GKV_E_ARG).
+ * A graded entry's code * scale + zero is rounded to fp16 at most once (where few rows
+ * attend, the scales are applied apart and it is not) and probabilities enter the value
+ * product in fp16; logits, maxima and sums are fp32.  A token that a row does not see has
+ * no effect on it, whatever it holds.  n_new_host[b] is at most the sequence's length
+ * (GKV_E_SHAPE) and 0 for a retired one (GKV_E_ARG).  Lengths and levels are those of the
+ * host mirrors at the call; a captured call replays for them.
  * ws: gkv_chunk_ws_bytes(c, n_new_host) bytes (16-byte aligned, no initialisation; may be
  * NULL when that is 0), which depends on the lengths (-1: the call would be refused).
  * GKV_E_UNSUPPORTED for more than GKV_MAX_CHUNK_SEQS sequences. */

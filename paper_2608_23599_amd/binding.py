@@ -6,7 +6,8 @@ path runs in the library's HIP kernels.  The library must be built
 
 The function names mirror the C calls (``quantize_block``, ``demote``,
 ``page_boxes``, ``quest_select``, ``graded_decode_attn``, ``rd_residual_select``,
-``append``); ``GradedCache`` owns the device tables and the slab arena of one
+``append``; for many queries ``prompt_attn``, ``append_chunk``, ``truncate``,
+``chunk_attn``); ``GradedCache`` owns the device tables and the slab arena of one
 layer's cache and marshals them into the ``gkv_cache`` descriptor.
 """
 import contextlib
@@ -262,7 +263,7 @@ def _rows_out(out, n, h, dtype, device, what):
 def _int_list(lens, n, what, bits):
     """lens as a list of n plain ints that `bits` bits hold (an int: the same n times)."""
     if type(lens) is not list or any(type(x) is not int for x in lens):
-        a = np.asarray(lens)
+        a = lens.cpu().numpy() if isinstance(lens, torch.Tensor) else np.asarray(lens)
         if a.dtype.kind not in "iu" and a.size:
             raise GkvError(-2, what)
         if a.ndim == 0 and n is not None:
@@ -715,6 +716,7 @@ class GradedCache:
     def chunk_attn(self, q, lens, out=None, ws=None):
         """gkv_chunk_attn: attention of the lens[b] newest tokens of every sequence over the
         cache they were appended to (q packed fp16 rows [n][Hq][128], n = sum of lens).
+        ws: a contiguous uint8 workspace of gkv_chunk_ws_bytes, by default one of this call.
         Returns out [n][Hq][128] fp16."""
         q, n, _, qs = _rows_dev(q, "chunk_attn", self.Hq, self._dev)
         lens = _int_list(lens, self.B, "chunk_attn", 32)
@@ -723,6 +725,8 @@ class GradedCache:
         if sum(lens) != n:
             raise GkvError(-2, "chunk_attn")
         out, os = _rows_out(out, n, self.Hq, torch.float16, self._dev, "chunk_attn")
+        if ws is not None and (ws.dtype != torch.uint8 or ws.device != self._dev or not ws.is_contiguous()):
+            raise GkvError(-1, "chunk_attn")
         arr = (_i32 * self.B)(*lens)
         if ws is None:
             # of this call alone: its size goes by the lengths, and a captured graph keeps its own

@@ -44,8 +44,7 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr int kRows = 32;          // rows of a wavefront
-constexpr float kRescale = 8.0f;   // lazy rescale threshold (log2 units)
+constexpr float kRescale = 8.0f;  // lazy rescale threshold (log2 units)
 
 struct F16 {
   static constexpr uint32_t kInf = 0x7C00u, kExp = 0x7C007C00u;  // infinity; the exponent bits of a pair

@@ -468,6 +468,147 @@ def test_workspaces_streams_and_graphs(gpu):
         assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("newest", [16, 8])
+def test_contexts_past_every_count(gpu, newest):
+    """A million tokens a head, blocks that repeat a few records (as many of each, so that the
+    output is that of one of each): lists of more blocks than a wavefront reads table entries
+    of at once, tiles past 4 GB."""
+    import torch
+    Hq, Hkv, order = 16, 8, [0, 1, 2, 4, 8, 16]
+    order = [x for x in order if x != newest] + [newest]
+    small = Case(gpu, 81, (64 * 6,), (0,), Hq, Hkv, lambda T: np.array(order, np.int8), ragged=False)
+    times = 2834
+    c = small.cache
+    big = gpu.GradedCache(1, Hkv, Hq, 64 * 6 * times, 6 * times, {16: 1})
+    big.arena = c.arena
+    for name in ("level_host", "koff_host", "voff_host"):
+        getattr(big, name)[:] = np.tile(getattr(c, name)[:, :, :6], (1, 1, times))
+    big._bind(64 * 6 * times, 0)
+    big._upload_tables()
+    q = synth.rng(81, 2, 3).standard_normal((1, Hq, 128), dtype=np.float32).astype(np.float16)
+    out = big.chunk_attn(q.view(np.uint16), [1]).float().cpu().numpy()
+    del big
+    torch.cuda.empty_cache()
+    for g in range(Hq):
+        kh, vh = small.units[0, g // 2].khat_vhat()
+        ref, tol = rows_reference(q.view(np.uint16)[:, g], kh, vh, [383], np.zeros(384, bool))
+        # (fp32 sums of a million weights, of which a wavefront's are some 4000 one after the other)
+        tol = tol + 4096 * 2.0 ** -24 * (np.abs(vh).max() + np.abs(ref))
+        assert (np.abs(out[:, g] - ref) / tol).max() <= 1.0, g
+
+
+@pytest.mark.gpu
+def test_rows_and_records_past_32_bits(gpu):
+    """Tokens' rows 2 MB apart and slots behind 4 GB."""
+    import torch
+    T, Hq, Hkv = 2200, 4, 2
+    ks, vs = kv_all(83, 1, Hkv, T)
+    q, k, v = (torch.randn(T, Hq, 128).half().cuda(),
+               *(torch.from_numpy(np.ascontiguousarray(x[0].transpose(1, 0, 2)).view(np.int16)).view(torch.float16).cuda()
+                 for x in (ks, vs)))
+    want = gpu.prompt_attn(q, k, v, [T])
+    wide = torch.zeros(T, 1 << 20, dtype=torch.float16, device="cuda")
+    assert wide.numel() > 1 << 31
+    parts, at = [], 0
+    for x in (q, k, v, torch.zeros_like(q)):
+        view = wide[:, at:at + x.shape[1] * 128].unflatten(1, (x.shape[1], 128))
+        view.copy_(x)
+        parts.append(view)
+        at += x.shape[1] * 128
+    qw, kw, vw, out = parts
+    gpu.prompt_attn(qw, kw, vw, [T], out=out)
+    assert torch.equal(out, want)
+    cache = gpu.GradedCache(1, Hkv, Hq, 0, 40, {16: 300000}, seq_lens=[0])
+    cache.pool.alloc_many(16, 300000 - 2 * Hkv * 40)
+    cache.append_chunk(kw, vw, [T])
+    assert int(cache.koff_host[0, 0, 0]) > 1 << 32
+    out.zero_()
+    cache.chunk_attn(qw, [T], out=out)
+    assert float((out.float() - want.float()).abs().max()) <= 4e-3
+    near = cache.chunk_attn(q, [T])
+    assert torch.equal(out, near)
+    few = cache.chunk_attn(qw[-3:], [3])
+    assert float((few.float() - want[-3:].float()).abs().max()) <= 4e-3
+    assert torch.equal(few, cache.chunk_attn(q[-3:], [3]))
+    cache.truncate([64 * 34])
+    assert int((cache.record(0, 1, 33, 0)["values"] != ofp16.to_f64(ks[0, 1, 64 * 33:64 * 34])).sum()) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,n,nres", [(64 * 130, 100, 0), (64 * 81, 65, 0), (64 * 96 + 7, 130, 900), (64 * 20, 70, 1100)])
+def test_one_centroid_tiles(gpu, T, n, nres):
+    """One-centroid blocks by the tile: more than 64, 64 and fewer, and blocks of which residual
+    rows leave nothing."""
+    c = Case(gpu, 85, (T,), (n,), 4, 2, "rdv2", nres=nres, ragged=False)
+    c.check(c.run())
+    m = min(n, 9)  # and the few-row form over the same cache
+    q = c.q[n - m:]
+    c.check(c.cache.chunk_attn(np.ascontiguousarray(q).view(np.uint16), [m]), [m])
+
+
+@pytest.mark.gpu
+def test_many_sequences(gpu):
+    """128 sequences, idle, short, of single tokens and of chunks, both forms in one call."""
+    r = np.random.default_rng(87)
+    lens, news = r.integers(0, 260, 128), r.choice([0, 1, 2, 7, 150], 128, p=[0.2, 0.3, 0.2, 0.2, 0.1])
+    lens[:3], news[:3] = (0, 64 * 70, -1), (0, 150, 0)
+    c = Case(gpu, 87, lens, news, 2, 1, "tiny")
+    c.check(c.run())
+
+
+@pytest.mark.gpu
+def test_calls_at_once(gpu):
+    """Two streams, each with a cache of its own and one shared, the default workspaces."""
+    import torch
+    cs = [Case(gpu, 89 + i, (64 * 50 + 3, 400), (40, 3), 8, 2, "graded") for i in range(3)]
+    qs = [torch.from_numpy(c.q).cuda() for c in cs]
+    for c in cs:
+        c.append()
+    want = [c.cache.chunk_attn(q, c.news) for c, q in zip(cs, qs)]
+    cs[0].check(want[0])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got += [(j, cs[j].cache.chunk_attn(qs[j], torch.tensor(cs[j].news))) for j in (i, 2)]
+        torch.cuda.synchronize()
+        for j, out in got:
+            assert torch.equal(out, want[j])
+
+
+@pytest.mark.gpu
+def test_binding_refusals(gpu):
+    """Arguments that the binding or the library turns away; the cache is as it was."""
+    import torch
+    c = Case(gpu, 91, (64 * 40, 70), (3, 2), 4, 2, "graded")
+    k, v = (torch.from_numpy(x.view(np.int16)).view(torch.float16).cuda() for x in c.new_rows())
+    q, cache = torch.from_numpy(c.q).cuda(), c.cache
+    for a in ((k[:-1], v, c.news), (k, v[:, :1], c.news), (k.bfloat16(), v, c.news), (k, v, [3]), (k, v, [3.0, 2.0]),
+              (k, v, [6, -1]), (k, v, [1 << 40, 2]), (k, v, [5])):
+        with pytest.raises(gpu.GkvError):
+            cache.append_chunk(*a)
+    assert cache.lengths().tolist() == c.lens
+    c.append()
+    need = int(gpu._chunk_ws(gpu.ctypes.byref(cache.c), np.array(c.news, np.int32).ctypes.data))
+    assert need > 0
+    empty = lambda n, t=torch.uint8: torch.empty(n, dtype=t, device="cuda")
+    for a, kw in (((q, [3, 3]), {}), ((q[:, :3], c.news), {}), ((q.bfloat16(), c.news), {}), ((q, [5, 0, 0]), {}),
+                  ((q, c.news), {"ws": empty(need - 1)}), ((q, c.news), {"ws": empty(need, torch.float32)}),
+                  ((q, c.news), {"ws": empty(2 * need)[::2]}), ((q, c.news), {"out": q.float()}),
+                  ((q, c.news), {"out": torch.empty_like(q).transpose(0, 1)}),
+                  ((q, c.news), {"out": empty(5 * 512, torch.float16).as_strided((5, 4, 128), (256, 128, 1))})):
+        with pytest.raises(gpu.GkvError):
+            cache.chunk_attn(*a, **kw)
+    with pytest.raises(gpu.GkvError):
+        cache.truncate([64 * 40])
+    want = cache.chunk_attn(q, c.news)
+    c.check(want)
+    assert torch.equal(want, cache.chunk_attn(q, np.array(c.news), ws=empty(need)))
+
+
 # ---------------------------------------------------------------- refusals (host only)
 
 
@@ -537,6 +678,8 @@ def test_chunk_attn_refusals(host):
     lens[1] = -1
     assert call((0, 1)) == (-1, -1)
     lens[1] = 5
+    big = np.full((2, 2, 4096), 16, np.int8)
+    c.level_host = big.ctypes.data
     c.nblk_cap, c.T = 4096, 64 * 4096
     lens[0] = 64 * 4096
     nb = call((1, 1))[1]
