@@ -131,46 +131,39 @@ __device__ __forceinline__ void load_raw(Raw &x, const uint8_t *rec, int level, 
 }
 
 // Codes 2 q and 2 q + 1 of a chunk under a fixed exponent, 2^k + code in fp16 (exact), and that
-// power of two; words 2 c and 2 c + 1 have the same one.  kNear: at most 64 (but for eight bits), for
-// a shift more; see few_kernel.
-template <int BITS, bool kNear = false>
+// power of two; words 2 c and 2 c + 1 have the same one.  It is small (but for eight bits): where the
+// codes are multiplied as they are, it is part of every product and taken off the sum.
+template <int BITS>
 __device__ __forceinline__ uint32_t raw_offset(int q) {
   if constexpr (BITS == 8) return 0x64006400u;
-  if constexpr (BITS == 4) return !(q & 2) ? 0x54005400u : kNear ? 0x4C004C00u : 0x64006400u;
-  const uint32_t e[4] = {0x44004400u, 0x4C004C00u, 0x54005400u, kNear ? 0x44004400u : 0x64006400u};
+  if constexpr (BITS == 4) return (q & 2) ? 0x4C004C00u : 0x54005400u;
+  const uint32_t e[4] = {0x44004400u, 0x4C004C00u, 0x54005400u, 0x44004400u};
   return e[(q & 7) >> 1];
 }
 // The exponents in vector registers, behind the compiler's back: an and-or takes one constant that
 // is not in one, and as literals they make it two instructions.
 struct Exponents {
-  uint32_t e[4];  // 4, 16, 64, 1024
-  __device__ __forceinline__ Exponents() {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      e[i] = raw_offset<2>(2 * i);
-      asm("" : "+v"(e[i]));
-    }
+  uint32_t e4, e16, e64, e1024;
+  __device__ __forceinline__ Exponents() : e4(0x44004400u), e16(0x4C004C00u), e64(0x54005400u), e1024(0x64006400u) {
+    asm("" : "+v"(e4), "+v"(e16), "+v"(e64), "+v"(e1024));
   }
 };
-template <int BITS, bool kNear = false>
+template <int BITS>
 __device__ __forceinline__ uint32_t raw_pair(const u4 (&w)[4], int q, const Exponents &x) {
   const bool odd = q & 1;
   if constexpr (BITS == 8) {
-    return __builtin_amdgcn_perm(x.e[3], w[q >> 3][(q >> 1) & 3], odd ? 0x07030702u : 0x07010700u);
+    return __builtin_amdgcn_perm(x.e1024, w[q >> 3][(q >> 1) & 3], odd ? 0x07030702u : 0x07010700u);
   } else if constexpr (BITS == 4) {
     const uint32_t y = w[0][q >> 2];
-    if (!(q & 2)) return ((odd ? y >> 8 : y) & 0x00F000F0u) | x.e[2];
-    if (kNear) return ((odd ? y >> 2 : y << 6) & 0x03C003C0u) | x.e[1];
-    return ((odd ? y >> 8 : y) & 0x000F000Fu) | x.e[3];
+    if (q & 2) return ((odd ? y >> 2 : y << 6) & 0x03C003C0u) | x.e16;
+    return ((odd ? y >> 8 : y) & 0x00F000F0u) | x.e64;
   } else {
     const uint32_t y = w[0][q >> 3];
     switch (q & 7) {
-      case 0: case 1: return ((odd ? y >> 6 : y) & 0x03000300u) | x.e[0];
-      case 2: case 3: return ((odd ? y >> 6 : y) & 0x00C000C0u) | x.e[1];
-      case 4: case 5: return ((odd ? y >> 6 : y) & 0x00300030u) | x.e[2];
-      default:
-        if (kNear) return ((odd ? y << 6 : y << 8) & 0x03000300u) | x.e[0];
-        return ((odd ? y >> 2 : y) & 0x00030003u) | x.e[3];
+      case 0: case 1: return ((odd ? y >> 6 : y) & 0x03000300u) | x.e4;
+      case 2: case 3: return ((odd ? y >> 6 : y) & 0x00C000C0u) | x.e16;
+      case 4: case 5: return ((odd ? y >> 6 : y) & 0x00300030u) | x.e64;
+      default: return ((odd ? y << 6 : y << 8) & 0x03000300u) | x.e4;
     }
   }
 }
@@ -650,8 +643,9 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams 
 //   q . k = sum (2^k + code) (q s) + sum z q - sum 2^k (q s), with q s as two fp16 terms and the
 //   constant part from the matrix units too, for any token the same;
 //   sum p v = s (sum p (2^k + code) - 2^k sum p) + z sum p, once a step.
-// Both sums are held in 32 bits, where 2^k <= 1024 costs 2^-14 of a code's step at most; the values'
-// are near theirs (16 and 64 for four bits), as what a long context leaves of them is small.  The rows of
+// Both sums are held in 32 bits, of which 2^k takes some: it is 1024 for eight bits, 16 and 64 for four, 4 to
+// 64 for two (with the 1024 that costs a shift less, 2 tokens over 128k were off by 7e-4 of their
+// outputs' size, which a long context leaves small, and now by 2.5e-4, as fp16 outputs are).  The rows of
 // q are brought below 1 and s is at most 65504 2 / 3 (two bits), 8734 or 514, so that no q s
 // overflows; those of eight bits are raised by 2^6, so that the second term of one is lost only
 // where 2^-12 of the code's span is less than a step of fp16's smallest numbers.
@@ -848,7 +842,7 @@ __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half,
       Raw w;
       few_codes<LEVEL>(w, buf, 2 * pp + g, lane);
 #pragma unroll
-      for (int q = 0; q < 16; ++q) a[q >> 1][2 * g + (q & 1)] = raw_pair<LEVEL, true>(w.w, q, e);
+      for (int q = 0; q < 16; ++q) a[q >> 1][2 * g + (q & 1)] = raw_pair<LEVEL>(w.w, q, e);
     }
     if (vtok) {  // scales of tokens: into the values here
 #pragma unroll
@@ -858,7 +852,7 @@ __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half,
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
           const uint32_t y = a[q >> 1][2 * g + (q & 1)];
-          a[q >> 1][2 * g + (q & 1)] = decoded(halves(y) - halves(raw_offset<LEVEL, true>(q)), s[q & 1], z[q & 1]);
+          a[q >> 1][2 * g + (q & 1)] = decoded(halves(y) - halves(raw_offset<LEVEL>(q)), s[q & 1], z[q & 1]);
         }
       }
     }
@@ -1105,9 +1099,9 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParam
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c) {  // (repeats after four)
-      const uint32_t off = x.level == GKV_INT8   ? raw_offset<8, true>(2 * (c & 3))
-                           : x.level == GKV_INT4 ? raw_offset<4, true>(2 * (c & 3))
-                                                 : raw_offset<2, true>(2 * (c & 3));
+      const uint32_t off = x.level == GKV_INT8   ? raw_offset<8>(2 * (c & 3))
+                           : x.level == GKV_INT4 ? raw_offset<4>(2 * (c & 3))
+                                                 : raw_offset<2>(2 * (c & 3));
       const float z = scaled ? -(float)halves(off)[0] * sum : 0.f;
       acc[c] = c < 4 ? f4{z, z, z, z} : acc[c & 3];
     }
