@@ -364,20 +364,6 @@ __device__ __forceinline__ void load_queries(u4 (&q)[8], const ChunkParams &p, c
   for (int d = 0; d < 8; ++d) q[d] = *(const u4 *)(qp + 16 * d);
 }
 
-__device__ __forceinline__ void store_row(const ChunkParams &p, const Job &j, int tok, int g, const ta::Rows &st,
-                                          float inv, int hf) {
-  uint16_t *op = p.out + (j.row0 + tok) * p.os + (int64_t)(j.h * p.G + g) * D + 4 * hf;
-#pragma unroll
-  for (int c = 0; c < 4; ++c)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      u2 w;
-      w[0] = T16::pack(st.o[c][4 * i] * inv, st.o[c][4 * i + 1] * inv);
-      w[1] = T16::pack(st.o[c][4 * i + 2] * inv, st.o[c][4 * i + 3] * inv);
-      *(u2 *)(op + 32 * c + 8 * i) = w;
-    }
-}
-
 __device__ __forceinline__ void store_part(float *part, const ta::Rows &st, float l, int hf) {
 #pragma unroll
   for (int c = 0; c < 4; ++c)
@@ -621,7 +607,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams 
         [&] { load_queries(q, p, j, tok, g, ln.hf); });
   const float l = st.l + ta::other_half(st.l);
   if (row >= j.rows) return;
-  if (split == 1) store_row(p, j, tok, g, st, l > 0.f ? 1.f / l : l, ln.hf);
+  if (split == 1)
+    ta::store_row<T16>(p.out + (j.row0 + tok) * p.os + (int64_t)(j.h * p.G + g) * D, st, l > 0.f ? 1.f / l : l, ln.hf);
   else store_part(p.part + (part_row(p, j, kTileRows) + 32 * wave + ln.col) * kPart, st, l, ln.hf);
 }
 

@@ -88,20 +88,9 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParam
 #pragma unroll
         for (int d = 0; d < 8; ++d) q[d] = *(const ta::u4 *)(qp + 16 * d);
       });
-  if (row < rows) {
-    const float l = st.l + ta::other_half(st.l);
-    const float inv = l > 0.f ? 1.f / l : l;  // (a NaN stays)
-    uint16_t *op = p.out + (start + tok) * p.os + (int64_t)(h * G + g) * D + 4 * ln.hf;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ta::u2 w;
-        w[0] = T::pack(st.o[c][4 * i] * inv, st.o[c][4 * i + 1] * inv);
-        w[1] = T::pack(st.o[c][4 * i + 2] * inv, st.o[c][4 * i + 3] * inv);
-        *(ta::u2 *)(op + 32 * c + 8 * i) = w;
-      }
-  }
+  const float l = st.l + ta::other_half(st.l);
+  const float inv = l > 0.f ? 1.f / l : l;  // (a NaN stays)
+  if (row < rows) ta::store_row<T>(p.out + (start + tok) * p.os + (int64_t)(h * G + g) * D, st, inv, ln.hf);
 }
 
 }  // namespace

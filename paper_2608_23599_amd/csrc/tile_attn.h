@@ -358,6 +358,28 @@ __device__ __forceinline__ void multiply(Rows &r, f16v (&s)[2], const Lane &ln, 
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// A row's outputs, O / l, from its first element on.  The halves of a row's lanes exchange the
+// quarters of two 8-channel groups, so that each stores 16 bytes.
+template <class T>
+__device__ __forceinline__ void store_row(uint16_t *row, const Rows &r, float inv, int hf) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      u4 w;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const u2 x = __builtin_bit_cast(
+            u2, __builtin_amdgcn_permlane32_swap(
+                    T::pack(r.o[c][4 * i + 2 * k] * inv, r.o[c][4 * i + 2 * k + 1] * inv),
+                    T::pack(r.o[c][4 * i + 4 + 2 * k] * inv, r.o[c][4 * i + 5 + 2 * k] * inv), false, false));
+        w[k] = x[0];
+        w[2 + k] = x[1];
+      }
+      *(u4 *)(row + 32 * c + 8 * (i + hf)) = w;
+    }
+}
+
 // ---------------------------------------------------------------- a workgroup's pass
 constexpr int kTile = 64;                  // tokens of a tile
 constexpr int kTileBytes = kTile * 128 * 2;  // of its keys, or of its values
