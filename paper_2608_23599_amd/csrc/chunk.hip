@@ -27,7 +27,7 @@ using ta::u4;
 using T16 = ta::F16;
 
 constexpr int kMaxSeqs = GKV_MAX_CHUNK_SEQS;
-constexpr int kPart = D + 2;  // floats of a row's partial: O, m, l
+constexpr int kPart = D + 4;  // floats of a row's partial: O, m, l, none twice (16-byte rows)
 
 struct ChunkParams {
   const uint16_t *q;
@@ -368,12 +368,9 @@ __device__ __forceinline__ void store_part(float *part, const ta::Rows &st, floa
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float4 w = make_float4(st.o[c][4 * i], st.o[c][4 * i + 1], st.o[c][4 * i + 2], st.o[c][4 * i + 3]);
-      float2 *d = (float2 *)(part + 32 * c + 8 * i + 4 * hf);
-      d[0] = make_float2(w.x, w.y);
-      d[1] = make_float2(w.z, w.w);
-    }
+    for (int i = 0; i < 4; ++i)
+      *(float4 *)(part + 32 * c + 8 * i + 4 * hf) =
+          make_float4(st.o[c][4 * i], st.o[c][4 * i + 1], st.o[c][4 * i + 2], st.o[c][4 * i + 3]);
   if (!hf) *(float2 *)(part + D) = make_float2(st.m, l);
 }
 
@@ -1166,10 +1163,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParam
   } else {
     float *part = p.part + (part_row(p, j, kFewRows) + m) * kPart;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      *(float2 *)(part + 16 * c + 4 * kg) = make_float2(r.o[c][0], r.o[c][1]);
-      *(float2 *)(part + 16 * c + 4 * kg + 2) = make_float2(r.o[c][2], r.o[c][3]);
-    }
+    for (int c = 0; c < 8; ++c) *(f4 *)(part + 16 * c + 4 * kg) = r.o[c];
     if (kg == 0) *(float2 *)(part + D) = make_float2(r.m, r.l);
   }
 }
@@ -1207,15 +1201,13 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, i
   for (int i = 0; i < n; ++i) {
     const float *x = part + i * step;
     const float2 ml = *(const float2 *)(x + D);
-    float2 y[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = *(const float2 *)(x + 8 * lane + 2 * k);
+    const f4 y0 = *(const f4 *)(x + 8 * lane), y1 = *(const f4 *)(x + 8 * lane + 4);
     const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
     l += f * ml.y;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      o[2 * k] += f * y[k].x;
-      o[2 * k + 1] += f * y[k].y;
+      o[k] += f * y0[k];
+      o[4 + k] += f * y1[k];
     }
   }
   const float inv = l > 0.f ? 1.f / l : l;
