@@ -386,10 +386,15 @@ constexpr int kTileBytes = kTile * 128 * 2;  // of its keys, or of its values
 constexpr int kBiasBytes = kTile * 4;
 constexpr int kAttendLds = 4 * kTileBytes;   // two tiles; with biases 2 kBiasBytes more
 
-// LDS copies of 16 bytes a lane, lane after lane from a wave-uniform LDS address.
+// LDS copies of 16 bytes a lane, lane after lane from a wave-uniform LDS address.  The compiler puts
+// no wait states in front of inline assembly: the base goes through a scalar move, as a vector
+// memory instruction must not follow closely on a vector instruction that wrote its scalar operand
+// (v_readlane), and that move stands between the write of M0 and its use.
 __device__ __forceinline__ void dma16(uint32_t voff, const void *base, uint32_t lds) {
   const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(m0v) : "memory", "m0");
+  uint64_t at;
+  asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0"
+               : "=&s"(at) : "v"(voff), "s"(base), "s"(m0v) : "memory", "m0");
 }
 
 // The rows of a workgroup over tiles t0 .. t1 - 1 (t0 < t1), those before `full` seen whole by
