@@ -10,7 +10,6 @@ The function names mirror the C calls (``quantize_block``, ``demote``,
 ``chunk_attn``); ``GradedCache`` owns the device tables and the slab arena of one
 layer's cache and marshals them into the ``gkv_cache`` descriptor.
 """
-import contextlib
 import ctypes
 import os
 
@@ -153,12 +152,14 @@ def _stream():
     return _raw_stream(torch.cuda.current_device())
 
 
-_HERE = contextlib.nullcontext()
-
-
-def _on(device):
-    """Makes a device the current one for a call (nothing where it is)."""
-    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+def _call_on(device, f, *args):
+    """f(*args, stream) on a device and its current stream; returns the status.  (Where the device is
+    the current one, as ever in a process with one, without a context's host time.)"""
+    i = device.index
+    if i == torch.cuda.current_device():
+        return f(*args, _stream() if _raw_stream is None else _raw_stream(i))
+    with torch.cuda.device(device):
+        return f(*args, _stream())
 
 
 def block_bytes(level):
@@ -238,6 +239,8 @@ def _rows_dev(x, what, heads=None, device=None):
         x = x.to(device if device is not None else "cuda")
     if n == 0:
         return x, n, h, h * D
+    if x.is_contiguous() and x.data_ptr() % 16 == 0:
+        return x, n, h, h * D
     st, sh, se = x.stride()
     if n == 1:  # (a single row's stride is of no matter)
         st = h * D
@@ -249,11 +252,12 @@ def _rows_dev(x, what, heads=None, device=None):
     return x, n, h, st
 
 
-def _rows_out(out, n, h, dtype, device, what):
-    """The rows a call writes, new or the caller's, and the elements between two tokens' rows."""
-    if out is None:
-        return torch.empty((n, h, D), dtype=dtype, device=device), h * D
-    if out.shape != (n, h, D) or out.dtype != dtype or out.device != device:
+def _rows_out(out, q, what):
+    """The rows a call writes, like q's, new or the caller's, and the elements between two tokens' rows."""
+    n, h, _ = q.shape
+    if out is None:  # (dense, which empty_like is where q is)
+        return torch.empty_like(q) if q.is_contiguous() else q.new_empty((n, h, D)), h * D
+    if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
         raise GkvError(-2, what)
     if n and (out.stride(2) != 1 or h > 1 and out.stride(1) != D):
         raise GkvError(-2, what)
@@ -291,10 +295,10 @@ def prompt_attn(q, k, v, lens, out=None):
         raise GkvError(-2, "prompt_attn")
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise GkvError(-1, "prompt_attn")
-    out, os = _rows_out(out, n, Hq, q.dtype, dev, "prompt_attn")
-    with _on(dev):
-        _check(_prompt_attn(_dptr(q), _dptr(k), _dptr(v), _dptr(out), int(q.dtype == torch.bfloat16), Hkv, Hq,
-                            len(lens), (_i64 * len(lens))(*lens), qs, ks, vs, os, _stream()), "prompt_attn")
+    out, os = _rows_out(out, q, "prompt_attn")
+    _check(_call_on(dev, _prompt_attn, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                    int(q.dtype == torch.bfloat16), Hkv, Hq, len(lens), (_i64 * len(lens))(*lens), qs, ks, vs, os),
+           "prompt_attn")
     return out
 
 
@@ -690,9 +694,8 @@ class GradedCache:
         if slots:
             kv = self.pool.alloc_many(EXACT, 2 * slots)
             nk, nv = kv[0::2].copy(), kv[1::2].copy()
-        with _on(self._dev):
-            st = _append_chunk(ctypes.byref(self.c), _dptr(kd), _dptr(vd), ks, vs, (_i32 * self.B)(*lens),
-                               _np_ptr(nk) if slots else None, _np_ptr(nv) if slots else None, slots, _stream())
+        st = _call_on(self._dev, _append_chunk, ctypes.byref(self.c), kd.data_ptr(), vd.data_ptr(), ks, vs,
+                      (_i32 * self.B)(*lens), _np_ptr(nk) if slots else None, _np_ptr(nv) if slots else None, slots)
         if st != 0:
             if slots:
                 for off in kv[::-1]:
@@ -709,9 +712,8 @@ class GradedCache:
     def truncate(self, lens):
         """gkv_truncate: every sequence keeps its first lens[b] tokens (-1 for a retired one)."""
         lens = _int_list(lens, self.B, "truncate", 64)
-        with _on(self._dev):
-            _check(_truncate(ctypes.byref(self.c), self.pool.h, self.koff_host.ctypes.data,
-                             self.voff_host.ctypes.data, (_i64 * self.B)(*lens), _stream()), "truncate")
+        _check(_call_on(self._dev, _truncate, ctypes.byref(self.c), self.pool.h, _np_ptr(self.koff_host),
+                        _np_ptr(self.voff_host), (_i64 * self.B)(*lens)), "truncate")
 
     def chunk_attn(self, q, lens, out=None, ws=None):
         """gkv_chunk_attn: attention of the lens[b] newest tokens of every sequence over the
@@ -724,7 +726,7 @@ class GradedCache:
             raise GkvError(-1, "chunk_attn")
         if sum(lens) != n:
             raise GkvError(-2, "chunk_attn")
-        out, os = _rows_out(out, n, self.Hq, torch.float16, self._dev, "chunk_attn")
+        out, os = _rows_out(out, q, "chunk_attn")
         if ws is not None and (ws.dtype != torch.uint8 or ws.device != self._dev or not ws.is_contiguous()):
             raise GkvError(-1, "chunk_attn")
         arr = (_i32 * self.B)(*lens)
@@ -732,9 +734,8 @@ class GradedCache:
             # of this call alone: its size goes by the lengths, and a captured graph keeps its own
             nb = _chunk_ws(ctypes.byref(self.c), arr)
             ws = torch.empty(nb, dtype=torch.uint8, device=self._dev) if nb > 0 else None
-        with _on(self._dev):
-            _check(_chunk_attn(_dptr(q), qs, ctypes.byref(self.c), arr, _dptr(out), os, _dptr(ws),
-                               ws.numel() if ws is not None else 0, _stream()), "chunk_attn")
+        _check(_call_on(self._dev, _chunk_attn, q.data_ptr(), qs, ctypes.byref(self.c), arr, out.data_ptr(), os,
+                        _dptr(ws), ws.numel() if ws is not None else 0), "chunk_attn")
         return out
 
     def quest_select(self, q, topk, out=None):
