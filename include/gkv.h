@@ -409,7 +409,8 @@ gkv_status gkv_rd_residual_select(gkv_cache *c, const uint16_t *k_src, const uin
  * fp32; probabilities enter the value product, and outputs are stored, rounded to the
  * type.  A token that a row does not see has no effect on it, whatever its key and value
  * hold (infinities and NaN included).  GKV_E_UNSUPPORTED for more than GKV_MAX_PROMPTS
- * prompts or GKV_MAX_PROMPT_TOKENS tokens in one call. */
+ * prompts or GKV_MAX_PROMPT_TOKENS tokens in one call, or rows past 2^32 threads of one
+ * launch (two for a row). */
 typedef enum gkv_dtype { GKV_F16 = 0, GKV_BF16 = 1 } gkv_dtype;
 #define GKV_MAX_PROMPTS 256
 #define GKV_MAX_PROMPT_TOKENS 100000000
@@ -462,7 +463,8 @@ gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, 
  * host mirrors at the call; a captured call replays for them.
  * ws: gkv_chunk_ws_bytes(c, n_new_host) bytes (16-byte aligned, no initialisation; may be
  * NULL when that is 0), which depends on the lengths (-1: the call would be refused).
- * GKV_E_UNSUPPORTED for more than GKV_MAX_CHUNK_SEQS sequences. */
+ * GKV_E_UNSUPPORTED for more than GKV_MAX_CHUNK_SEQS sequences, or lengths past 2^32 threads
+ * of one launch (four for a token of the longest). */
 int64_t gkv_chunk_ws_bytes(const gkv_cache *c, const int32_t *n_new_host);
 gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const gkv_cache *c, const int32_t *n_new_host,
                           uint16_t *out, int64_t out_stride, void *ws, int64_t ws_bytes, void *stream);

@@ -249,7 +249,7 @@ static gkv_status append_chunk(gkv_cache *c, const uint16_t *k_new, const uint16
   }
   if (opened != n_open) return GKV_E_ARG;
   if (!rows) return GKV_OK;
-  if (items > 0x7fffffff || c->Hkv > 65535) return GKV_E_UNSUPPORTED;
+  if (items > GKV_MAX_LAUNCH / kThreads || c->Hkv > 65535) return GKV_E_UNSUPPORTED;
   if (!k_new || !v_new || (uintptr_t)k_new % 16 || (uintptr_t)v_new % 16) return GKV_E_ARG;
   for (const int64_t s : {k_stride, v_stride}) {
     if (s < (int64_t)c->Hkv * D) return GKV_E_SHAPE;

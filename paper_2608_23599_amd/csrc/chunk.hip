@@ -1288,7 +1288,7 @@ gkv_status plan_part(Part &t, const gkv_cache *c, int64_t fill) {
     if (s > 1) t.merged += (int64_t)p.n[i] * G;
     t.wgs += s * tiles(i);
     t.tiles += blocks(i) * c->Hkv;
-    if (t.wgs * c->Hkv > 0x7fffffff || t.tiles > 0x7fffffff) return GKV_E_UNSUPPORTED;
+    if (t.wgs * c->Hkv > GKV_MAX_LAUNCH / 512 || t.tiles > 0x7fffffff) return GKV_E_UNSUPPORTED;
   }
   p.wg0[p.nseq] = (int32_t)t.wgs;
   t.part_rows = t.merged ? t.wgs * c->Hkv * t.rows_tile : 0;
@@ -1310,7 +1310,9 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
     if (!n) continue;
     if (T < 0) return GKV_E_ARG;
     if (n > T) return GKV_E_SHAPE;
-    if (T > 0x7fffff00 || n * G > 0x7fffff00 || rows + n > 0x7fffffff) return GKV_E_UNSUPPORTED;
+    if (T > 0x7fffff00 || n * G > 0x7fffff00 || rows + n > 0x7fffffff ||
+        list_tiles((int)T, c->nres) > GKV_MAX_LAUNCH / 256)
+      return GKV_E_UNSUPPORTED;
     bool few = n * G <= kFewMost;  // and the blocks that some row sees in part are exact
     for (int h = 0; h < c->Hkv && few; ++h)
       for (int64_t i = (T - n) / P; i < (T + P - 1) / P; ++i)

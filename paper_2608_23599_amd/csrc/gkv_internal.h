@@ -139,6 +139,9 @@ GKV_HD double f16_to_f64(uint16_t h) {
 
 }  // namespace gkv
 
+// Threads that one launch takes along a dimension.
+constexpr int64_t GKV_MAX_LAUNCH = 0xffffffff;
+
 // Host-side validation shared by the call wrappers (host.cpp).
 gkv_status gkv_validate_cache(const gkv_cache *c);
 

@@ -153,7 +153,7 @@ extern "C" gkv_status gkv_prompt_attn(const void *q, const void *k, const void *
     tiles += (seqs[i].first * G + 32 * kWaves - 1) / (32 * kWaves);
   }
   p.tiles[n] = (int32_t)tiles;
-  if (tiles * Hkv > 0x7fffffff) return GKV_E_UNSUPPORTED;
+  if (tiles * Hkv > GKV_MAX_LAUNCH / (64 * kWaves)) return GKV_E_UNSUPPORTED;
   const dim3 grid((unsigned)(tiles * Hkv)), blk(64 * kWaves);
   const size_t lds = ta::kAttendLds;
   if (dtype == GKV_F16)

@@ -684,6 +684,11 @@ def test_chunk_attn_refusals(host):
     lens[0] = 64 * 4096
     nb = call((1, 1))[1]
     assert nb > 0 and call((1, 1))[0] == -1 and call((1, 1), ws=4096, ws_bytes=nb - 1)[0] == -4
+    huge = np.full((1, 1, 1 << 25), 16, np.int8)  # more threads than a launch takes
+    c.B = c.Hkv = c.Hq = 1
+    c.level_host, c.nblk_cap = huge.ctypes.data, 1 << 25
+    c.T = lens[0] = 1 << 31 - 1
+    assert call((1, 0), ws=4096, ws_bytes=1 << 50) == (-6, -1)
 
 
 def test_truncate_refusals(host):

@@ -226,6 +226,7 @@ def test_refusals():
     assert _call(B, ptr=4104) == -1
     assert _call(B, lens=(1,) * 257) == -6
     assert _call(B, lens=(100000000, 1)) == -6
+    assert _call(B, Hkv=64, Hq=64, lens=(100000000,)) == -6  # more threads than a launch takes
 
 
 def test_binding_refusals():
