@@ -697,12 +697,15 @@ __device__ __forceinline__ float over_groups(float x) {  // the maximum over a r
 }
 
 // Scores to packed probabilities (two words a page), raising the maxima as tile_attn.h does.
-__device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, const f4 (&s)[4], float sl2) {
+__device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, f4 (&s)[4], float sl2) {
   float top = -__builtin_inff();
 #pragma unroll
   for (int g = 0; g < 4; ++g)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, __builtin_fmaf(s[g][i], sl2, -r.m));
+    for (int i = 0; i < 4; ++i) {
+      s[g][i] = __builtin_fmaf(s[g][i], sl2, -r.m);
+      top = fmaxf(top, s[g][i]);
+    }
   if (__builtin_expect(__any(top > r.raise), 0)) {
     const float high = over_groups(top);
     const bool mine = high > r.raise;
@@ -713,15 +716,14 @@ __device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, const 
     r.l *= f;
 #pragma unroll
     for (int c = 0; c < 8; ++c) r.o[c] *= f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) s[g] -= up;
   }
 #pragma unroll
   for (int g = 0; g < 4; ++g)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * i], sl2, -r.m));
-      const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * i + 1], sl2, -r.m));
-      p[2 * g + i] = T16::pack(a, b);
-    }
+    for (int i = 0; i < 2; ++i)
+      p[2 * g + i] = T16::pack(__builtin_amdgcn_exp2f(s[g][2 * i]), __builtin_amdgcn_exp2f(s[g][2 * i + 1]));
 }
 
 // Copies of a record (exact: of its pages 2 half, 2 half + 1) to LDS.
