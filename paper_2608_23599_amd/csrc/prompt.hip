@@ -46,11 +46,11 @@ struct PromptTiles {
   __device__ __forceinline__ void values(int t, uint32_t lds) const { copy(t, lds, v, vs, false); }
 };
 
-// One workgroup for 32 WAVES rows of a (prompt, KV head), 215 registers and 64 KB of LDS: one on a
-// compute unit, two wavefronts a SIMD.  Bound by matrix and vector issue beside one another (1.87 us
+// One workgroup for 32 WAVES rows of a (prompt, KV head), up to 220 registers and 64 KB of LDS: two
+// wavefronts a SIMD, in one workgroup or two (see launch).  Bound by matrix and vector issue beside one another (1.87 us
 // for 256 rows x 64 tokens), and in short prompts by the first copies, masked tiles and stores, about
-// 6 us a workgroup with nothing else on its unit.  28/4 heads in bf16: one prompt of 16k tokens
-// 1790 us (1.08 PFLOP/s; a large library product reaches 1.27), sixteen of 107 to 2000 220 us;
+// 6 us a workgroup of eight wavefronts with nothing else on its unit.  28/4 heads in bf16: one prompt of 16k tokens
+// 1790 us (1.08 PFLOP/s; a large library product reaches 1.27), sixteen of 107 to 2000 207 us;
 // 32/8 heads in fp16, 4k tokens: 148 us.
 template <class T, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParams p) {
@@ -99,6 +99,40 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParam
   if (row < rows) ta::store_row<T>(p.out + (start + tok) * p.os + (int64_t)(h * G + g) * D, st, inv, ln.hf);
 }
 
+// Row tiles of every sequence at so many rows each; returns their number.
+int64_t row_tiles(PromptParams &p, int rows) {
+  int64_t tiles = 0;
+  for (int i = 0; i < p.nseq; ++i) {
+    p.tiles[i] = (int32_t)tiles;
+    tiles += ((int64_t)p.len[i] * p.G + rows - 1) / rows;
+  }
+  p.tiles[p.nseq] = (int32_t)tiles;
+  return tiles;
+}
+
+// Eight wavefronts a workgroup, or four, of which a compute unit holds two: those share no tiles, so that
+// a step takes 5% longer, but one works through the other's first copies and stores, and half as
+// many rows leave fewer units idle.  Four: up to 128 workgroups of eight (28/4 heads, one prompt
+// of 512 tokens 19.6 us against 23.7, 1000 tokens 31 against 37); up to 256, one a unit, where row
+// tiles are of many lengths (2000 tokens 54 against 65, but four prompts of 512 26.3 against 26.1
+// and with 32/8 heads 27.6 against 25.0); beyond, where they are short (64 x 128 tokens 45 against
+// 60, 16 x 1000 171 against 181, but 16 x 3000 1205 against 1174, one of 4096 145 against 136).
+template <class T>
+gkv_status launch(PromptParams &p, hipStream_t s) {
+  const int64_t wide = row_tiles(p, 256) * p.Hkv;
+  int64_t steps = 0;  // of 64 tokens, over all row tiles (twice)
+  for (int i = 0; i < p.nseq; ++i) steps += (int64_t)(p.tiles[i + 1] - p.tiles[i]) * (p.len[i] / ta::kTile + 1);
+  steps = steps * p.Hkv / (2 * wide);
+  const bool narrow = wide <= 128 || (wide <= 256 ? steps >= 8 : steps <= 12);
+  const int64_t wgs = narrow ? row_tiles(p, 128) * p.Hkv : wide;
+  const int threads = narrow ? 256 : 512;
+  if (wgs > GKV_MAX_LAUNCH / threads) return GKV_E_UNSUPPORTED;
+  const dim3 grid((unsigned)wgs), blk(threads);
+  if (narrow) hipLaunchKernelGGL((prompt_kernel<T, 4>), grid, blk, ta::kAttendLds, s, p);
+  else hipLaunchKernelGGL((prompt_kernel<T, 8>), grid, blk, ta::kAttendLds, s, p);
+  return hipGetLastError() == hipSuccess ? GKV_OK : GKV_E_HIP;
+}
+
 }  // namespace
 
 extern "C" gkv_status gkv_prompt_attn(const void *q, const void *k, const void *v, void *out, int32_t dtype,
@@ -144,21 +178,9 @@ extern "C" gkv_status gkv_prompt_attn(const void *q, const void *k, const void *
   p.G = G;
   p.nseq = n;
   p.sl2 = 1.4426950408889634f / sqrtf((float)D);
-  constexpr int kWaves = 8;
-  int64_t tiles = 0;
   for (int i = 0; i < n; ++i) {
     p.len[i] = (int32_t)seqs[i].first;
     p.start[i] = (int32_t)seqs[i].second;
-    p.tiles[i] = (int32_t)tiles;
-    tiles += (seqs[i].first * G + 32 * kWaves - 1) / (32 * kWaves);
   }
-  p.tiles[n] = (int32_t)tiles;
-  if (tiles * Hkv > GKV_MAX_LAUNCH / (64 * kWaves)) return GKV_E_UNSUPPORTED;
-  const dim3 grid((unsigned)(tiles * Hkv)), blk(64 * kWaves);
-  const size_t lds = ta::kAttendLds;
-  if (dtype == GKV_F16)
-    hipLaunchKernelGGL((prompt_kernel<ta::F16, kWaves>), grid, blk, lds, (hipStream_t)stream, p);
-  else
-    hipLaunchKernelGGL((prompt_kernel<ta::BF16, kWaves>), grid, blk, lds, (hipStream_t)stream, p);
-  return hipGetLastError() == hipSuccess ? GKV_OK : GKV_E_HIP;
+  return dtype == GKV_F16 ? launch<ta::F16>(p, (hipStream_t)stream) : launch<ta::BF16>(p, (hipStream_t)stream);
 }

@@ -199,6 +199,28 @@ def test_streams_and_graphs(gpu):
         assert torch.equal(out, gpu.prompt_attn(q, k, v, lens))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("odd", [False, True])
+def test_both_widths_of_a_workgroup(gpu, dtype, odd):
+    """Long prompts together (row tiles of 256) and one by one (of 128): the same outputs, also where
+    tokens hold infinities and NaN."""
+    import torch
+    lens = [2000, 1777, 1, 64, 1999]
+    q, k, v = (x.cuda() for x in make(29, lens, 32, 8, dtype))
+    if odd:
+        for i, (at, x) in enumerate(((1900, float("inf")), (1950, float("nan")), (2000 + 1700, -float("inf")),
+                                     (2000 + 1776, float("nan")))):
+            (v if i % 2 == 0 else k)[at, i, 5 * i] = x
+    got, at = gpu.prompt_attn(q, k, v, lens), 0
+    for n in lens:
+        one = gpu.prompt_attn(q[at:at + n], k[at:at + n], v[at:at + n], [n])
+        same = (got[at:at + n] == one) | (got[at:at + n].isnan() & one.isnan())
+        assert bool(same.all())
+        assert odd or not bool(one.isnan().any())
+        at += n
+
+
 def _call(B, dtype=0, Hkv=2, Hq=4, lens=(5, 3), strides=None, ptr=4096, null=None):
     import ctypes
     lens = np.array(lens, dtype=np.int64)
