@@ -407,7 +407,7 @@ gkv_status gkv_rd_residual_select(gkv_cache *c, const uint16_t *k_src, const uin
  * (GKV_E_SHAPE) and at most GKV_MAX_ROW_STRIDE (GKV_E_UNSUPPORTED).  Lengths may be 0 (the
  * prompt has no rows).  out must not overlap the inputs.  Logits, maxima and sums are
  * fp32; probabilities enter the value product, and outputs are stored, rounded to the
- * type.  A token that a row does not see has no effect on it, whatever its key and value
+ * type (in fp16 one below 2^-32 of the row's largest is 0).  A token that a row does not see has no effect on it, whatever its key and value
  * hold (infinities and NaN included).  GKV_E_UNSUPPORTED for more than GKV_MAX_PROMPTS
  * prompts or GKV_MAX_PROMPT_TOKENS tokens in one call, or rows past 2^32 threads of one
  * launch (two for a row). */
@@ -457,7 +457,8 @@ gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, 
  * elements from token to token (rules as for gkv_prompt_attn); out must not overlap q.
  * A graded entry's code * scale + zero is rounded to fp16 at most once (where few rows
  * attend, the scales are applied apart and it is not) and probabilities enter the value
- * product in fp16; logits, maxima and sums are fp32.  A token that a row does not see has
+ * product in fp16 (one below 2^-32 of the largest that a share of the context holds is 0);
+ * logits, maxima and sums are fp32.  A token that a row does not see has
  * no effect on it, whatever it holds.  n_new_host[b] is at most the sequence's length
  * (GKV_E_SHAPE) and 0 for a retired one (GKV_E_ARG).  Lengths and levels are those of the
  * host mirrors at the call; a captured call replays for them.

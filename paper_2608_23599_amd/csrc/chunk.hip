@@ -696,7 +696,7 @@ __device__ __forceinline__ float over_groups(float x) {  // the maximum over a r
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
-// Scores to packed probabilities (two words a page), raising the maxima as tile_attn.h does.
+// Scores to packed probabilities (two words a page), moving the references as tile_attn.h does.
 __device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, f4 (&s)[4], float sl2) {
   float top = -__builtin_inff();
 #pragma unroll
@@ -709,7 +709,7 @@ __device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, f4 (&s
   if (__builtin_expect(__any(top > r.raise), 0)) {
     const float high = over_groups(top);
     const bool mine = high > r.raise;
-    const float up = mine ? high : 0.f;
+    const float up = mine ? high - ta::kLead : 0.f;
     const float f = r.raise < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
     r.raise = mine ? ta::kRescale : r.raise;
     r.m += up;

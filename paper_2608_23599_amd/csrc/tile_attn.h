@@ -17,10 +17,14 @@
 // same order: the probabilities never leave their lane.  O^T has a row per lane too, so the
 // rescale by a new maximum is one factor per lane.
 //
-// The running maximum is only raised when some score passes it by more than kRescale
-// (2^8): probabilities stay below 2^8 (far inside fp16), the sums are in fp32 and the
-// common tile has no cross-lane step.  Probabilities enter the second product in the
-// type of the values (one rounding of at most half a step each); the sum of a row adds
+// Weights are taken relative to a reference that is set kLead (2^7) below the largest score so
+// far and only moved when a score passes it by more than kRescale (2^15): the largest weight of a
+// row lies between 2^7 and 2^15, the sums are in fp32 and the common tile has no cross-lane step.
+// So fp16 weights use the type's range on both sides: they stay below its 65504, are normal
+// numbers down to 2^-21 of the largest one and vanish below 2^-32 of it.  (With the reference at
+// the largest score itself they vanished below 2^-25: beside one token that took nearly all of a
+// row's weight, 16384 others of together 5e-4 were lost.)  Weights enter the second product
+// in the type of the values (one rounding of at most half a step each); the sum of a row adds
 // the rounded ones, so the weights of a row sum to 1 as the product sees them.
 //
 // A masked score becomes -infinity by selection, never by arithmetic, so a NaN or infinity
@@ -44,7 +48,8 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr float kRescale = 8.0f;  // lazy rescale threshold (log2 units)
+constexpr float kRescale = 15.0f;  // an exponent above this moves the reference (log2 units)
+constexpr float kLead = 7.0f;      // the largest one's exponent when it has moved
 
 struct F16 {
   static constexpr uint32_t kInf = 0x7C00u, kExp = 0x7C007C00u;  // infinity; the exponent bits of a pair
@@ -211,7 +216,7 @@ __device__ __forceinline__ void mask_scores(f16v (&s)[NT], const Lane &ln, uint6
   }
 }
 
-// Raises the maxima where a score passes one by more than kRescale, and turns scores into
+// Moves the references where a score passes one by more than kRescale, and turns scores into
 // packed probabilities (two 16-token pages a group).
 template <class T, int NT>
 __device__ __forceinline__ void weights(u4 (&p)[2 * NT], Rows &r, const f16v (&s)[NT], float sl2) {
@@ -228,7 +233,7 @@ __device__ __forceinline__ void weights(u4 (&p)[2 * NT], Rows &r, const f16v (&s
     // so that a row's rounding does not depend on its neighbours'
     const float high = fmaxf(top, other_half(top));
     const bool go = high > r.raise;
-    const float up = go ? high : 0.f;
+    const float up = go ? high - kLead : 0.f;
     const float f = r.raise < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
     r.raise = go ? kRescale : r.raise;
     r.m += up;
