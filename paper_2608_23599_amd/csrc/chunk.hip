@@ -819,11 +819,13 @@ __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half,
   const int kg = lane >> 4, m = lane & 15;
   // word q of page g's chunk (tokens 4 kg + 2 (q & 1) and the next, channel 16 (q >> 1) + m) is
   // a[q >> 1][2 g + (q & 1)]
-  if constexpr (LEVEL == GKV_MEAN) {  // the one key's place alone
+  // A token that is read elsewhere has weight 0, but 0 * infinity is NaN: its values become zeros
+  // (but where scales are of channels: what those decode to is infinite or NaN for every token).
+  if constexpr (LEVEL == GKV_MEAN) {  // the one key's place alone, if it stands for any token
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
       const uint32_t v = lds_u16(buf + 2 * (16 * c + m));
-      a[c] = u4{lane < 16 ? v : 0, 0, 0, 0};
+      a[c] = u4{lane < 16 && x.drop != ~0ull ? v : 0, 0, 0, 0};
     }
   } else if constexpr (is_codes(LEVEL)) {
 #pragma unroll
@@ -838,11 +840,15 @@ __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half,
       for (int g = 0; g < 2; ++g) {
         const uint32_t at = buf + (16 * (2 * pp + g) + 4 * kg) * 2;
         const u2 s = *(LdsW2)(uintptr_t)at, z = *(LdsW2)(uintptr_t)(at + 128);
+        uint32_t y[16];
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
-          const uint32_t y = a[q >> 1][2 * g + (q & 1)];
-          a[q >> 1][2 * g + (q & 1)] = decoded(halves(y) - halves(raw_offset<LEVEL>(q)), s[q & 1], z[q & 1]);
+          const uint32_t w = a[q >> 1][2 * g + (q & 1)];
+          y[q] = decoded(halves(w) - halves(raw_offset<LEVEL>(q)), s[q & 1], z[q & 1]);
         }
+        if (x.drop) drop_words(y, x.drop, 2 * pp + g, kg);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) a[q >> 1][2 * g + (q & 1)] = y[q];
       }
     }
   } else {
@@ -863,8 +869,6 @@ __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half,
           for (int i = 0; i < 4; ++i) y[4 * j + i] = b[i];
         }
       }
-      // a token that is read elsewhere has weight 0, but 0 * infinity is NaN (an integer
-      // block's infinities and NaN are those of whole channels)
       if (x.drop) drop_words(y, x.drop, 2 * (half + pp) + g, kg);
 #pragma unroll
       for (int q = 0; q < 16; ++q) a[q >> 1][2 * g + (q & 1)] = y[q];
@@ -1108,7 +1112,9 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) few_kernel(const ChunkParam
         for (int c = 0; c < 8; ++c)
           acc[c] = mfma16(a[c], u4{w[4 * pp], w[4 * pp + 1], w[4 * pp + 2], w[4 * pp + 3]}, acc[c]);
       }
-    if (scaled) {  // channels 16 c + 4 kg .. + 3 lie side by side in the header's lane order
+    if (scaled && x.drop == ~0ull) {
+      // no token of it is read here: sums of zeros, which an infinite scale would make NaN
+    } else if (scaled) {  // channels 16 c + 4 kg .. + 3 lie side by side in the header's lane order
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const u4 sc = ta::lds_u4(vbuf + kg * 64 + h * 16), z = ta::lds_u4(vbuf + 256 + kg * 64 + h * 16);
