@@ -697,14 +697,15 @@ __device__ __forceinline__ float over_groups(float x) {  // the maximum over a r
 }
 
 // Scores to packed probabilities (two words a page), moving the references as tile_attn.h does.
-__device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, f4 (&s)[4], float sl2) {
+__device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, const f4 (&s)[4], float sl2) {
   float top = -__builtin_inff();
+  f4 x[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[g][i] = __builtin_fmaf(s[g][i], sl2, -r.m);
-      top = fmaxf(top, s[g][i]);
+      x[g][i] = __builtin_fmaf(s[g][i], sl2, -r.m);
+      top = fmaxf(top, x[g][i]);
     }
   if (__builtin_expect(__any(top > r.raise), 0)) {
     const float high = over_groups(top);
@@ -716,14 +717,18 @@ __device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, f4 (&s
     r.l *= f;
 #pragma unroll
     for (int c = 0; c < 8; ++c) r.o[c] *= f;
+    // formed from the scores again: with the move taken off the exponents above they would keep the
+    // rounding of large ones (in a wavefront's first block those of the whole score)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) s[g] -= up;
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[g][i] = __builtin_fmaf(s[g][i], sl2, -r.m);
   }
 #pragma unroll
   for (int g = 0; g < 4; ++g)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      p[2 * g + i] = T16::pack(__builtin_amdgcn_exp2f(s[g][2 * i]), __builtin_amdgcn_exp2f(s[g][2 * i + 1]));
+      p[2 * g + i] = T16::pack(__builtin_amdgcn_exp2f(x[g][2 * i]), __builtin_amdgcn_exp2f(x[g][2 * i + 1]));
 }
 
 // Copies of a record (exact: of its pages 2 half, 2 half + 1) to LDS.
