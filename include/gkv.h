@@ -455,8 +455,9 @@ gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, 
  *   out[i][g][:] = sum_{j <= t} softmax_j(q_ig . k_j / sqrt(128)) v_j.
  * q, out: packed rows of [Hq][128] fp16, sequence after sequence, q_stride / out_stride
  * elements from token to token (rules as for gkv_prompt_attn); out must not overlap q.
- * A graded entry's code * scale + zero is rounded to fp16 at most once (where few rows
- * attend, the scales are applied apart and it is not) and probabilities enter the value
+ * A graded entry's code * scale + zero is rounded to fp16 at most once, to 65504 if that is
+ * less (where up to 128 rows of a sequence attend, scales per channel are applied apart and it
+ * is not rounded) and probabilities enter the value
  * product in fp16 (one below 2^-32 of the largest that a share of the context holds is 0);
  * logits, maxima and sums are fp32.  A token that a row does not see has
  * no effect on it, whatever it holds.  n_new_host[b] is at most the sequence's length

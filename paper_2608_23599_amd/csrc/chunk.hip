@@ -204,6 +204,24 @@ __device__ __forceinline__ uint32_t decoded(half2v code, uint32_t scale, uint32_
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, halves(scale), halves(zero)));
 }
 
+// Entries past the largest fp16 number, which codes of values next to it can stand for (eight bits, values
+// 0 .. 65504: 255 * 257), are that number: as infinities they would make whole outputs infinite or
+// NaN.  What an infinite scale or zero, or a NaN, decodes to stays as it is.
+template <int BITS, class Pairs>
+__device__ __forceinline__ bool past_fp16(const Pairs &scales, const Pairs &zeros) {  // (or not a number, in some lane)
+  half2v most;
+  most[0] = most[1] = (_Float16)(float)((1 << BITS) - 1);
+  float zero = 0.f;
+#pragma unroll
+  for (uint32_t i = 0; i < sizeof(Pairs) / 4; ++i) zero = T16::times0(decoded(most, scales[i], zeros[i]), zero);
+  return __any(zero != zero);
+}
+__device__ __forceinline__ uint32_t bounded(uint32_t y, uint32_t scale, uint32_t zero) {
+  const uint32_t off = ta::bad_halves<T16>(scale) | ta::bad_halves<T16>(zero);  // halves that stay
+  const uint32_t lo = (y & 0xFFFFu) == T16::kInf ? 1u : 0u, hi = y >> 16 == T16::kInf ? 0x10000u : 0u;
+  return y - ((lo | hi) & ~off);
+}
+
 template <int BITS>
 __device__ __forceinline__ void stage_key_codes(uint32_t (&y)[16], const Raw &x, uint32_t head, int kg, const Exponents &e) {
 #pragma unroll
@@ -211,6 +229,9 @@ __device__ __forceinline__ void stage_key_codes(uint32_t (&y)[16], const Raw &x,
     const u4 s = ta::lds_u4(head + kg * 64 + j * 16), z = ta::lds_u4(head + 256 + kg * 64 + j * 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[4 * j + i] = decoded(code_pair<BITS>(x.w, 4 * j + i, e), s[i], z[i]);
+    if (__builtin_expect(past_fp16<BITS>(s, z), 0))
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[4 * j + i] = bounded(y[4 * j + i], s[i], z[i]);
   }
 }
 __device__ __forceinline__ half2v twice(uint32_t pair, int i) {
@@ -228,6 +249,9 @@ __device__ __forceinline__ void stage_value_codes(uint32_t (&y)[16], const Raw &
     const u2 z = *(LdsW2)(uintptr_t)(head + 512 + 128 + (16 * pg + 4 * kg) * 2);
 #pragma unroll
     for (int q = 0; q < 16; ++q) y[q] = decoded(code_pair<BITS>(x.w, q, e), s[q & 1], z[q & 1]);
+    if (__builtin_expect(past_fp16<BITS>(s, z), 0))
+#pragma unroll
+      for (int q = 0; q < 16; ++q) y[q] = bounded(y[q], s[q & 1], z[q & 1]);
   } else {
     const u4 s = ta::lds_u4(head + 512 + m * 16), z = ta::lds_u4(head + 768 + m * 16);
 #pragma unroll
@@ -237,6 +261,11 @@ __device__ __forceinline__ void stage_value_codes(uint32_t (&y)[16], const Raw &
                                 __builtin_elementwise_fma(code_pair<BITS>(x.w, q, e), twice(s[c >> 1], c & 1),
                                                           twice(z[c >> 1], c & 1)));
     }
+    if (__builtin_expect(past_fp16<BITS>(s, z), 0))
+#pragma unroll
+      for (int q = 0; q < 16; ++q)
+        y[q] = bounded(y[q], __builtin_bit_cast(uint32_t, twice(s[q >> 2], q >> 1 & 1)),
+                       __builtin_bit_cast(uint32_t, twice(z[q >> 2], q >> 1 & 1)));
   }
 }
 
@@ -851,6 +880,9 @@ __device__ __forceinline__ void few_values(u4 (&a)[8], const Visit &x, int half,
           const uint32_t w = a[q >> 1][2 * g + (q & 1)];
           y[q] = decoded(halves(w) - halves(raw_offset<LEVEL>(q)), s[q & 1], z[q & 1]);
         }
+        if (__builtin_expect(past_fp16<LEVEL>(s, z), 0))
+#pragma unroll
+          for (int q = 0; q < 16; ++q) y[q] = bounded(y[q], s[q & 1], z[q & 1]);
         if (x.drop) drop_words(y, x.drop, 2 * pp + g, kg);
 #pragma unroll
         for (int q = 0; q < 16; ++q) a[q >> 1][2 * g + (q & 1)] = y[q];
