@@ -152,9 +152,17 @@ def _stream():
     return _raw_stream(torch.cuda.current_device())
 
 
+def _on(device, f, *args):
+    """f(*args) with a device as the current one (as ever in a process with one: without a context's
+    host time)."""
+    if device.index == torch.cuda.current_device():
+        return f(*args)
+    with torch.cuda.device(device):
+        return f(*args)
+
+
 def _call_on(device, f, *args):
-    """f(*args, stream) on a device and its current stream; returns the status.  (Where the device is
-    the current one, as ever in a process with one, without a context's host time.)"""
+    """f(*args, stream) on a device and its current stream; returns the status."""
     i = device.index
     if i == torch.cuda.current_device():
         return f(*args, _stream() if _raw_stream is None else _raw_stream(i))
@@ -732,7 +740,7 @@ class GradedCache:
         arr = (_i32 * self.B)(*lens)
         if ws is None:
             # of this call alone: its size goes by the lengths, and a captured graph keeps its own
-            nb = _chunk_ws(ctypes.byref(self.c), arr)
+            nb = _on(self._dev, _chunk_ws, ctypes.byref(self.c), arr)
             ws = torch.empty(nb, dtype=torch.uint8, device=self._dev) if nb > 0 else None
         _check(_call_on(self._dev, _chunk_attn, q.data_ptr(), qs, ctypes.byref(self.c), arr, out.data_ptr(), os,
                         _dptr(ws), ws.numel() if ws is not None else 0), "chunk_attn")

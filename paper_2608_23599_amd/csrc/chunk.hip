@@ -1277,7 +1277,6 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const ChunkParams p, i
 // 89; 16 x 2000 25 and 51, 35 and 53, 45 and 57.
 constexpr int kFewMost = 128;
 constexpr int kLeastVisits = 4;  // blocks that a workgroup takes at least
-constexpr int64_t kCus = 256;
 
 // One launch's part of a call.
 struct Part {
@@ -1372,8 +1371,9 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
   }
   pl.few.rows_tile = kFewRows;
   pl.many.rows_tile = 256;
-  gkv_status st = plan_part(pl.few, c, 2 * kCus);
-  if (!st) st = plan_part(pl.many, c, kCus);
+  const int64_t cus = gkv_device_cus();
+  gkv_status st = plan_part(pl.few, c, 2 * cus);
+  if (!st) st = plan_part(pl.many, c, cus);
   if (st) return st;
   auto align = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
   pl.part = 0;

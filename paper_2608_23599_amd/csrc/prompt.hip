@@ -112,8 +112,8 @@ int64_t row_tiles(PromptParams &p, int rows) {
 
 // Eight wavefronts a workgroup, or four, of which a compute unit holds two: those share no tiles, so that
 // a step takes 5% longer, but one works through the other's first copies and stores, and half as
-// many rows leave fewer units idle.  Four: up to 128 workgroups of eight (28/4 heads, one prompt
-// of 512 tokens 19.6 us against 23.7, 1000 tokens 31 against 37); up to 256, one a unit, where row
+// many rows leave fewer units idle.  Four: up to half a workgroup of eight a unit (of 256; 28/4 heads, one prompt
+// of 512 tokens 19.6 us against 23.7, 1000 tokens 31 against 37); up to one a unit, where row
 // tiles are of many lengths (2000 tokens 54 against 65, but four prompts of 512 26.3 against 26.1
 // and with 32/8 heads 27.6 against 25.0); beyond, where they are short (64 x 128 tokens 45 against
 // 60, 16 x 1000 171 against 181, but 16 x 3000 1205 against 1174, one of 4096 145 against 136).
@@ -123,7 +123,8 @@ gkv_status launch(PromptParams &p, hipStream_t s) {
   int64_t steps = 0;  // of 64 tokens, over all row tiles (twice)
   for (int i = 0; i < p.nseq; ++i) steps += (int64_t)(p.tiles[i + 1] - p.tiles[i]) * (p.len[i] / ta::kTile + 1);
   steps = steps * p.Hkv / (2 * wide);
-  const bool narrow = wide <= 128 || (wide <= 256 ? steps >= 8 : steps <= 12);
+  const int64_t cus = gkv_device_cus();
+  const bool narrow = wide <= cus / 2 || (wide <= cus ? steps >= 8 : steps <= 12);
   const int64_t wgs = narrow ? row_tiles(p, 128) * p.Hkv : wide;
   const int threads = narrow ? 256 : 512;
   if (wgs > GKV_MAX_LAUNCH / threads) return GKV_E_UNSUPPORTED;
