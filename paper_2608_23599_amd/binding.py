@@ -617,7 +617,7 @@ class GradedCache:
         # keep forming runs of back-to-back records
         kv = self._take([int(t) for t in np.repeat(to, 2)])
         nk, nv = kv[0::2].copy(), kv[1::2].copy()
-        st = _demote(ctypes.byref(self.c), n, _np_ptr(J), _np_ptr(to), _np_ptr(nk), _np_ptr(nv), _stream())
+        st = _call_on(self._dev, _demote, ctypes.byref(self.c), n, _np_ptr(J), _np_ptr(to), _np_ptr(nk), _np_ptr(nv))
         if st != 0:
             for t, a, bb in zip(to, nk, nv):
                 self.pool.free(int(t), int(a))
