@@ -235,6 +235,8 @@ def _rows_dev(x, what, heads=None, device=None):
     whose heads lie side by side in 16-byte aligned rows is taken as it is, any other one is
     copied.  Returns the tensor, n, heads and the elements from a token's rows to the next's."""
     if isinstance(x, np.ndarray):
+        if x.dtype not in (np.float16, np.int16, np.uint16):
+            raise GkvError(-2, what)
         x = torch.from_numpy(np.ascontiguousarray(x).view(np.int16))
     if x.dtype == torch.int16:
         x = x.view(torch.float16)

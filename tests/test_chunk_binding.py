@@ -31,3 +31,13 @@ def test_demotions_run_on_the_caches_device(calls):
     c.demote([(0, 0, 0), (0, 0, 1)], [8, 8])
     assert calls == [(c._dev, B._demote)]
     assert c.pool.used(8) == 4 and c.pool.used(16) == 8
+
+
+@pytest.mark.parametrize("dtype", [np.float32, np.float64, np.int32, np.int64, np.uint8])
+def test_arrays_of_other_types_are_no_bit_patterns(dtype):
+    """Whose bytes would make rows of 128 halves."""
+    width = 256 // np.dtype(dtype).itemsize
+    with pytest.raises(B.GkvError):
+        B._rows_dev(np.zeros((3, 2, width), dtype), "prompt_attn")
+    with pytest.raises(B.GkvError):
+        B._rows_dev(np.zeros((3, 2, 128), dtype), "prompt_attn")
