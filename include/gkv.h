@@ -157,6 +157,9 @@ typedef struct gkv_cache {
                                 has T tokens.  The calls that change lengths keep both
                                 copies in step.                                         */
   int64_t *seq_len_host;     /* host mirror of seq_len (both NULL or both set)          */
+  int32_t truncated;         /* set by gkv_truncate when it drops blocks: some of those
+                                that stay may stand below their ladder's level at the
+                                shorter length, where gkv_ladder_crossings leaves them  */
 } gkv_cache;
 
 /* Stamps c->version with a new process-wide unique value: a caller that has written
@@ -191,7 +194,8 @@ gkv_status gkv_ladder_levels(int32_t profile, int64_t T, int8_t *levels_host, in
  * lengths every active sequence grows by T_new - c->T tokens and is compared with the
  * profile at its own new length (retired sequences are skipped).  Returns the number
  * of crossings (>= 0), or a negative gkv_status; GKV_E_NOT_MONOTONE if the profile
- * would raise any block's level. */
+ * would raise any block's level (in a truncated cache such a block stays as it is: it was
+ * demoted when it was older than it is now). */
 int32_t gkv_ladder_crossings(const gkv_cache *c, int32_t profile, int64_t T_new, int32_t *jobs_host,
                              int8_t *to_host, int32_t max_jobs);
 
@@ -441,7 +445,8 @@ gkv_status gkv_append_chunk(gkv_cache *c, const uint16_t *k_new, const uint16_t 
  * for all without per-sequence lengths).  The dropped blocks' slots (host offset mirrors
  * koff_host / voff_host [B][Hkv][nblk_cap]) go back to pool, the next append's first;
  * they are reusable by later work on `stream`.  The dropped rows of a block that stays
- * become zero; its certificate number vmax stays (a bound).  A block that stays without
+ * become zero; its certificate number vmax stays (a bound).  Blocks that were demoted stay
+ * demoted.  A block that stays without
  * being filled must be exact (GKV_E_SHAPE: tokens of a demoted block cannot be dropped
  * apart).  GKV_E_UNSUPPORTED for a cache with residual rows, which may be rows of
  * dropped tokens. */

@@ -43,6 +43,7 @@ class CacheStruct(ctypes.Structure):
         ("v_per_token", _i32),
         ("version", ctypes.c_uint64),
         ("seq_len", _vp), ("seq_len_host", _vp),
+        ("truncated", _i32),
     ]
 
 

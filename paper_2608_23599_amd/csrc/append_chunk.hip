@@ -387,6 +387,9 @@ extern "C" gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *
   for (int b = 0; b < c->B; ++b)
     if (c->seq_len_host) c->seq_len_host[b] = p.to[b];
   c->T = longest;
-  if (any_block) gkv_stamp(c);
+  if (any_block) {
+    c->truncated = 1;
+    gkv_stamp(c);
+  }
   return GKV_OK;
 }

@@ -111,7 +111,10 @@ extern "C" int32_t gkv_ladder_crossings(const gkv_cache *c, int32_t profile, int
         }
         const int cur = cl[i];
         if (lv[i] == cur) continue;
-        if (level_rank(lv[i]) > level_rank(cur)) return GKV_E_NOT_MONOTONE;
+        if (level_rank(lv[i]) > level_rank(cur)) {
+          if (c->truncated) continue;  // demoted when it was older
+          return GKV_E_NOT_MONOTONE;
+        }
         if (n < max_jobs) {
           jobs[3 * n] = b;
           jobs[3 * n + 1] = h;
