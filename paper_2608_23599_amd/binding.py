@@ -665,6 +665,29 @@ class GradedCache:
             self.voff_host[b, :, blk] = nv[b * self.Hkv:(b + 1) * self.Hkv]
         return self._cross(profile) if profile is not None else []
 
+    def _check_cross(self, profile, have, lens, what):
+        """Raises what the ladder's demotions would raise once sequences of have[b] tokens have lens[b]
+        more: blocks to be raised, or more slots than the pools have."""
+        need = np.zeros(EXACT + 1, np.int64)
+        ladders = {}
+        for b, (h, m) in enumerate(zip(have, lens)):
+            if h < 0 or m < 0 or h + m > P * self.nblk_cap:
+                continue  # retired, or what the append itself refuses
+            lv = ladders.get(h + m)
+            if lv is None:
+                lv = ladders[h + m] = ladder_levels(profile, h + m)
+            cur = self.level_host[b, :, :len(lv)]
+            old = -(-h // P)
+            if (lv[:old] > cur[:, :old]).any() and not self.c.truncated:
+                raise GkvError(-3, what)
+            if len(lv) > old:  # (the blocks that open are exact)
+                cur = cur.copy()
+                cur[:, old:] = EXACT
+            need += np.bincount(np.broadcast_to(lv, cur.shape)[lv < cur], minlength=EXACT + 1)
+        for i, level in enumerate(LEVELS):
+            if 2 * need[level] > self.pool._caps[i] - self.pool.used(level):
+                raise GkvError(-7, what)
+
     def _cross(self, profile):
         """Demotes every block whose level the ladder profile lowers at the present lengths;
         returns [(b, h, blk, old, new)]."""
@@ -687,8 +710,8 @@ class GradedCache:
     def append_chunk(self, k_new, v_new, lens, profile=None):
         """gkv_append_chunk: append lens[b] tokens to every sequence (k_new, v_new packed fp16
         rows [n][Hkv][128], n = sum of lens; views with a token stride are read in place);
-        then, with a ladder profile, demote what it lowers.  Returns the demotions
-        [(b, h, blk, old, new)]."""
+        then, with a ladder profile, demote what it lowers (checked before anything is appended).
+        Returns the demotions [(b, h, blk, old, new)]."""
         kd, n, _, ks = _rows_dev(k_new, "append_chunk", self.Hkv, self._dev)
         vd, nv, _, vs = _rows_dev(v_new, "append_chunk", self.Hkv, self._dev)
         lens = _int_list(lens, self.B, "append_chunk", 32)
@@ -697,6 +720,8 @@ class GradedCache:
         if nv != n or sum(lens) != n:
             raise GkvError(-2, "append_chunk")
         have = [self.T] * self.B if self.seq_len_host is None else self.seq_len_host.tolist()
+        if profile is not None:
+            self._check_cross(profile, have, lens, "append_chunk")
         # the blocks that open, (sequence, first, last): K and V slots of one block side by side
         opens = [(b, -(-h // P), -(-(h + m) // P)) for b, (h, m) in enumerate(zip(have, lens))
                  if m > 0 and h >= 0 and (h + m - 1) // P > (h - 1) // P]
