@@ -50,7 +50,7 @@ struct PromptTiles {
 // wavefronts a SIMD, in one workgroup or two (see launch).  Bound by matrix and vector issue beside one another (1.87 us
 // for 256 rows x 64 tokens), and in short prompts by the first copies, masked tiles and stores, about
 // 6 us a workgroup of eight wavefronts with nothing else on its unit.  28/4 heads in bf16: one prompt of 16k tokens
-// 1770 us (1.09 PFLOP/s; a large library product reaches 1.27), sixteen of 107 to 2000 207 to 220;
+// 1770 us (1.09 PFLOP/s; a large library product reaches 1.27), sixteen of 107 to 2000 210 to 226;
 // 32/8 heads in fp16, 4k tokens: 146 us.
 template <class T, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParams p) {
@@ -112,11 +112,14 @@ int64_t row_tiles(PromptParams &p, int rows) {
 
 // Eight wavefronts a workgroup, or four, of which a compute unit holds two: those share no tiles, so that
 // a step takes 5% longer, but one works through the other's first copies and stores, and half as
-// many rows leave fewer units idle.  Four: up to half a workgroup of eight a unit (of 256; 28/4 heads, one prompt
-// of 512 tokens 19.6 us against 23.7, 1000 tokens 31 against 37); up to one a unit, where row
-// tiles are of many lengths (2000 tokens 54 against 65, but four prompts of 512 26.3 against 26.1
-// and with 32/8 heads 27.6 against 25.0); beyond, where they are short (64 x 128 tokens 45 against
-// 60, 16 x 1000 171 against 181, but 16 x 3000 1205 against 1174, one of 4096 145 against 136).
+// many rows leave fewer units idle.  Four, in us against eight:
+//  * up to half a workgroup of eight a unit: 28/4 heads, one prompt of 512 tokens 19.6 and 23.7;
+//  * up to one a unit, where row tiles are of many lengths: one of 1200 to 2300 tokens 31.7 to 59.9 and
+//    40.1 to 69.2, but four of 512 26.3 and 26.1, with 32/8 heads 27.6 and 25.0;
+//  * beyond, where row tiles are short, up to 12 steps of 64 tokens on the mean.  Four over eight at 8
+//    steps 0.90 to 1.01, at 10 and 11 0.92 to 1.03 (sixteen prompts of 107 to 2000 tokens in bf16 209.7 and
+//    225.6), at 12 1.00 to 1.03, at 13 1.00 to 1.02, at 14 0.98 to 1.07, at 16 0.98 to 1.08, at 18
+//    1.02 to 1.09 (28/4 and 32/8 heads; one of 4096 at 32 steps 1.06 and 1.08).
 template <class T>
 gkv_status launch(PromptParams &p, hipStream_t s) {
   const int64_t wide = row_tiles(p, 256) * p.Hkv;
