@@ -7,8 +7,15 @@
 //    to LDS and decodes them into operands;
 //  * many rows: the cache is decoded once to fp16 tiles in the workspace, over which row tiles
 //    go as a prompt's do (tile_attn.h).
-// Either splits a long context over workgroups whose partials a merge kernel joins.  A graded
-// value is rounded to fp16 once, code * scale + zero in one step.
+// Either splits a long context over workgroups whose partials a merge kernel joins.
+//
+// A tile's entries are rounded to fp16 once, code * scale + zero in one step; of few rows only values with
+// scales per token are, all other scales go into the queries and outputs.  The rounding of the keys
+// is what shows: 0.7e-3 to 1.1e-3 of the outputs' size over a context of one level (normal keys with four
+// channels ten times larger), the values' 1.5e-4 to 2.0e-4, as the outputs' own (2.0e-4).  Rounded up or
+// down at random, tokens apart, both came to 1.1e-3: the outputs of a long context are themselves sums
+// in which the tokens' values cancel, so that errors that differ from token to token do not become
+// less beside them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -580,15 +587,16 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
   }
 }
 
+constexpr int kTileWaves = 8, kTileRows = 32 * kTileWaves;
+
 // A list's tiles: 1 KB a copy.
-template <int WAVES>
 struct ListTiles {
   const uint8_t *list;
   int wave, lane;
   __device__ __forceinline__ void copy(const uint8_t *src, uint32_t lds) const {
 #pragma unroll
-    for (int i = 0; i < 16 / WAVES; ++i) {
-      const uint32_t at = (wave + WAVES * i) * 1024;
+    for (int i = 0; i < 16 / kTileWaves; ++i) {
+      const uint32_t at = (wave + kTileWaves * i) * 1024;
       ta::dma16(lane * 16, src + at, lds + at);
     }
   }
@@ -602,13 +610,11 @@ struct ListTiles {
   }
 };
 
-// 32 WAVES rows over a share of a list, as a prompt's row tile (and as it bound by matrix and vector
+// 256 rows over a share of a list, as a prompt's row tile (and as it bound by matrix and vector
 // issue): 512 tokens x 28/4 heads over 64k 476 us (1.0 PFLOP/s).
-template <int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams p) {
+__global__ void __launch_bounds__(64 * kTileWaves, 2) tiles_kernel(const ChunkParams p) {
   extern __shared__ __align__(16) unsigned char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
-  constexpr int kTileRows = 32 * WAVES;
   const Job j = job_of(p, kTileRows, blockIdx.x % p.Hkv, blockIdx.x / p.Hkv);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   ta::Lane ln;
@@ -622,12 +628,12 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams 
   const int ntile = whole + last / P - c0 + 1;
   const int split = p.split[j.s];
   const int t0 = (int)((int64_t)ntile * j.part / split), t1 = (int)((int64_t)ntile * (j.part + 1) / split);
-  const ListTiles<WAVES> src = {p.list + (p.list0[j.s] + (int64_t)j.h * list_tiles(p, j.T)) * kListTile, wave, ln.lane};
+  const ListTiles src = {p.list + (p.list0[j.s] + (int64_t)j.h * list_tiles(p, j.T)) * kListTile, wave, ln.lane};
   ta::Rows st;
   u4 q[8];
   st.init();
   if (t0 < t1)  // (a row tile with fewer tiles than shares leaves some of them none)
-    ta::attend<T16, WAVES, false, true>(
+    ta::attend<T16, kTileWaves, false, true>(
         st, ln, q, lds, wave, t0, t1, whole + (first + 1) / P - c0, p.sl2, src,
         [&](int t) {  // this row's visible tokens of tile t
           const int n = t < whole ? P : j.pos0 + tok + 1 - (c0 + t - whole) * P;
@@ -662,7 +668,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tiles_kernel(const ChunkParams 
 // Both sums are held in 32 bits, of which 2^k takes some: it is 1024 for eight bits, 16 and 64 for four, 4 to
 // 64 for two (with the 1024 that costs a shift less, 2 tokens over 128k were off by 7e-4 of their
 // outputs' size, which a long context leaves small, and now by 2.5e-4, as fp16 outputs are).  The rows of
-// q are brought below 1 and s is at most 65504 2 / 3 (two bits), 8734 or 514, so that no q s
+// q are brought below 1 (a channel that is 2^-14 of its row's largest or less loses bits then, at most 2^-25 of
+// that largest) and s is at most 65504 2 / 3 (two bits), 8734 or 514, so that no q s
 // overflows; those of eight bits are raised by 2^6, so that the second term of one is lost only
 // where 2^-12 of the code's span is less than a step of fp16's smallest numbers.
 typedef float f4 __attribute__((ext_vector_type(4)));
@@ -1370,7 +1377,7 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
     rows += n;
   }
   pl.few.rows_tile = kFewRows;
-  pl.many.rows_tile = 256;
+  pl.many.rows_tile = kTileRows;
   const int64_t cus = gkv_device_cus();
   gkv_status st = plan_part(pl.few, c, 2 * cus);
   if (!st) st = plan_part(pl.many, c, cus);
@@ -1445,7 +1452,7 @@ extern "C" gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const 
       int most = 0;
       for (int i = 0; i < p.nseq; ++i) most = std::max(most, list_tiles(p.T[i], c->nres));
       hipLaunchKernelGGL(expand_kernel, dim3(most, c->Hkv, p.nseq), dim3(256), 0, s, p);
-      hipLaunchKernelGGL((tiles_kernel<8>), grid, dim3(512), ta::kAttendLds + 2 * ta::kBiasBytes, s, p);
+      hipLaunchKernelGGL(tiles_kernel, grid, dim3(64 * kTileWaves), ta::kAttendLds + 2 * ta::kBiasBytes, s, p);
     }
     if (hipGetLastError() != hipSuccess) return GKV_E_HIP;
     if (t->merged) {

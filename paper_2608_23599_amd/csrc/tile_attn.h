@@ -15,7 +15,7 @@
 // l & 31, tokens 8 (i >> 2) + 4 (l >> 5) + (i & 3)), which is, two values a register, the
 // layout of the second product's operand when its inner index runs over the tokens in that
 // same order: the probabilities never leave their lane.  O^T has a row per lane too, so the
-// rescale by a new maximum is one factor per lane.
+// rescale by a moved reference is one factor per lane.
 //
 // Weights are taken relative to a reference that is set kLead (2^7) below the largest score so
 // far and only moved when a score passes it by more than kRescale (2^15): the largest weight of a
@@ -28,7 +28,7 @@
 // the rounded ones, so the weights of a row sum to 1 as the product sees them.
 //
 // A masked score becomes -infinity by selection, never by arithmetic, so a NaN or infinity
-// in a masked key has no effect; for masked values see outputs_masked.
+// in a masked key has no effect; for masked values see find_odd.
 #pragma once
 
 #include <hip/hip_runtime.h>
