@@ -462,7 +462,8 @@ gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, 
  * elements from token to token (rules as for gkv_prompt_attn); out must not overlap q.
  * A graded entry's code * scale + zero is rounded to fp16 at most once, to 65504 if that is
  * less (where up to 128 rows of a sequence attend, scales per channel are applied apart and it
- * is not rounded) and probabilities enter the value
+ * is not rounded; where more do, the 16 channels of a KV head with the largest keys are held to
+ * 22 bits) and probabilities enter the value
  * product in fp16 (one below 2^-32 of the largest that a share of the context holds is 0);
  * logits, maxima and sums are fp32.  A token that a row does not see has
  * no effect on it, whatever it holds.  n_new_host[b] is at most the sequence's length
@@ -472,7 +473,7 @@ gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, 
  * NULL when that is 0), which depends on the lengths and on the current device's compute units
  * (-1: the call would be refused).  Where more than 128 rows of a sequence attend (or a block that one
  * sees in part is not exact) it holds the sequence's cache decoded, 33024 bytes for every block
- * and every 64 residual rows of a KV head.
+ * and every 64 residual rows of a KV head (35072 if one of them is an integer block).
  * GKV_E_UNSUPPORTED for more than GKV_MAX_CHUNK_SEQS sequences, or lengths past 2^32 threads
  * of one launch (four for a token of the longest). */
 int64_t gkv_chunk_ws_bytes(const gkv_cache *c, const int32_t *n_new_host);

@@ -9,13 +9,10 @@
 //    go as a prompt's do (tile_attn.h).
 // Either splits a long context over workgroups whose partials a merge kernel joins.
 //
-// A tile's entries are rounded to fp16 once, code * scale + zero in one step; of few rows only values with
-// scales per token are, all other scales go into the queries and outputs.  The rounding of the keys
-// is what shows: 0.7e-3 to 1.1e-3 of the outputs' size over a context of one level (normal keys with four
-// channels ten times larger), the values' 1.5e-4 to 2.0e-4, as the outputs' own (2.0e-4).  Rounded up or
-// down at random, tokens apart, both came to 1.1e-3: the outputs of a long context are themselves sums
-// in which the tokens' values cancel, so that errors that differ from token to token do not become
-// less beside them.
+// A tile's entries are rounded to fp16 once, code * scale + zero in one step, but for the keys' outlier
+// channels (see hot channels); of few rows only values with scales per token are, all other scales go into
+// the queries and outputs.  Outputs are then off by 0.3e-3 to 0.4e-3 of their size with many rows, 2.4e-4 to
+// 2.6e-4 with few, where the rounding of the outputs themselves takes 2.0e-4.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -52,6 +49,8 @@ struct ChunkParams {
   int64_t part0;             // first partial row of this launch
   uint8_t *list;             // many rows: the decoded tiles
   int32_t *whole;            // and how many of each list every row sees whole
+  uint8_t *hot;              // and each list's hot channels; bytes of a tile
+  int32_t tile;
   int32_t list0[kMaxSeqs];   // first tile of a sequence's lists (one a KV head)
   int32_t T[kMaxSeqs], n[kMaxSeqs];  // its tokens, and the newest ones that attend
   int32_t row0[kMaxSeqs];    // their first packed row
@@ -184,6 +183,10 @@ __device__ __forceinline__ half2v code_pair(const u4 (&w)[4], int q, const Expon
 typedef __attribute__((address_space(3))) u4 *LdsW4;
 typedef __attribute__((address_space(3))) u2 *LdsW2;
 typedef __attribute__((address_space(3))) uint32_t *LdsW1;
+
+__device__ __forceinline__ uint32_t lds_u16(uint32_t at) {
+  return *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)at;
+}
 
 // Scales and zeros in LDS: keys in the record's lane order (a lane's 32 are side by side);
 // values per channel as [channel & 15][channel >> 4], so that a lane's 8 are; values per
@@ -394,10 +397,20 @@ __device__ __forceinline__ int64_t part_row(const ChunkParams &p, const Job &j, 
   return p.part0 + ((int64_t)j.h * p.wg0[p.nseq] + p.wg0[j.s] + j.part * tiles + j.tile) * rows_tile;
 }
 
-__device__ __forceinline__ void load_queries(u4 (&q)[8], const ChunkParams &p, const Job &j, int tok, int g, int hf) {
-  const uint16_t *qp = p.q + (j.row0 + tok) * p.qs + (int64_t)(j.h * p.G + g) * D + 8 * hf;
+template <bool kRest, int NQ>
+__device__ __forceinline__ void load_queries(u4 (&q)[NQ], const ChunkParams &p, const Job &j, int tok, int g, int hf) {
+  const uint16_t *qp = p.q + (j.row0 + tok) * p.qs + (int64_t)(j.h * p.G + g) * D;
 #pragma unroll
-  for (int d = 0; d < 8; ++d) q[d] = *(const u4 *)(qp + 16 * d);
+  for (int d = 0; d < 8; ++d) q[d] = *(const u4 *)(qp + 16 * d + 8 * hf);
+  if constexpr (kRest) {  // the hot channels once more
+    const int64_t at = ((int64_t)j.s * p.Hkv + j.h) * (ta::kHot / 4);
+    const u4 ids = {table32(p.hot, at), table32(p.hot, at + 1), table32(p.hot, at + 2), table32(p.hot, at + 3)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = (hf ? ids[2 + (i >> 1)] : ids[i >> 1]) >> (16 * (i & 1));
+      q[8][i] = qp[two & 0xFF] | (uint32_t)qp[two >> 8 & 0xFF] << 16;
+    }
+  }
 }
 
 __device__ __forceinline__ void store_part(float *part, const ta::Rows &st, float l, int hf) {
@@ -443,7 +456,15 @@ __device__ __forceinline__ bool whole_at(const ChunkParams &p, const Job &j, int
 // A tile is 16 KB of keys, 16 KB of values and 64 floats that its scores start from: 0, minus
 // infinity for a place that holds no token (a residual token's in its block, those behind
 // the last row), log2(n) in a score's units for a one-centroid block, whose key counts for
-// its n tokens that are no residual ones.
+// its n tokens that are no residual ones.  Where a sequence of the call has integer blocks, 2 KB more: what the
+// rounding to fp16 took off the keys of the list's 16 hot channels, as operands of one more product.
+//
+// Hot channels are those of the largest keys (key channels are known to have outliers): a score's error is
+// that of its largest products.  With four channels ten times larger than the others the keys' rounding put the
+// outputs off by 0.7e-3 to 1.0e-3, over one level of codes, now by 2e-4.  (Rounding up or down at random,
+// tokens apart, came to 1.1e-3: a long context's outputs are themselves sums in which the tokens' values
+// cancel, so that errors that differ from token to token do not become less beside them.)  It costs a sixteenth
+// of the products: 512 tokens over 64k 568 us against 531, mixed chunks 313 against 287.
 constexpr int kListTile = 2 * ta::kTileBytes + ta::kBiasBytes;
 
 // Room of a list: a tile for every block and for every 64 residual rows.
@@ -463,8 +484,82 @@ __device__ __forceinline__ ListShape list_shape(const ChunkParams &p, int c0, in
   return l;
 }
 
-// One workgroup a block or 64 residual rows; a wavefront a page.  Bound by the bytes it writes: 47 us for
-// six sequences of 1343 to 12311 tokens x 8 KV heads (197 MB, 4.2 TB/s).
+// The hot channels of every list: the 16 with the largest keys in up to 16 integer blocks spread over the
+// context, by the ends of their ranges.  A thread a channel.  Bound by latency (three dependent round trips).
+__global__ void __launch_bounds__(D) hot_kernel(const ChunkParams p) {
+  constexpr int kSamples = 16;
+  __shared__ const _Float16 *heads[kSamples];
+  __shared__ float most[kSamples];  // a sample's largest code (0: no integer block)
+  __shared__ __align__(16) uint32_t size[D];
+  const int s = blockIdx.y, h = blockIdx.x, e = threadIdx.x;  // (e: place in a record's header)
+  const int nblk = (p.T[s] + P - 1) / P;
+  const int64_t u = (int64_t)p.seq[s] * p.Hkv + h;
+  int any = 0;
+  if (e < kSamples) {
+    const int64_t ti = u * p.nblk_cap + (int64_t)e * nblk / kSamples;
+    const int level = p.level[ti];
+    any = is_int_level(level);
+    heads[e] = (const _Float16 *)(p.arena + p.koff[ti]);
+    most[e] = any ? (float)((1 << level) - 1) : 0.f;
+  }
+  float sum = 0.f;
+  if (__syncthreads_or(any)) {
+    int last = 0;  // an integer block (the others' records may be shorter than a header)
+#pragma unroll
+    for (int i = 0; i < kSamples; ++i) last = most[i] != 0.f ? i : last;
+    float scale[kSamples], zero[kSamples];
+#pragma unroll
+    for (int i = 0; i < kSamples; ++i) {
+      const _Float16 *head = heads[most[i] != 0.f ? i : last];
+      scale[i] = (float)head[e];
+      zero[i] = (float)head[D + e];
+    }
+#pragma unroll
+    for (int i = 0; i < kSamples; ++i) {
+      const float end = __builtin_fmaf(most[i], scale[i], zero[i]);
+      sum += most[i] != 0.f ? fmaxf(zero[i] * zero[i], end * end) : 0.f;
+    }
+    sum = fminf(sum, 3e38f);  // (a NaN, too, is only large)
+  }
+  // sums that are no less than 0 compare as their bits do; the last seven tell channels apart
+  const int d = sz_channel(GKV_KEYS, e);
+  const uint32_t mine = (__builtin_bit_cast(uint32_t, sum) & ~127u) | d;
+  size[d] = mine;
+  __syncthreads();
+  int rank = 0;
+#pragma unroll
+  for (int i = 0; i < D / 4; ++i) {
+    const u4 x = *(const u4 *)(size + 4 * i);
+    rank += (x[0] > mine) + (x[1] > mine) + (x[2] > mine) + (x[3] > mine);
+  }
+  if (rank < ta::kHot) p.hot[((int64_t)s * p.Hkv + h) * ta::kHot + rank] = (uint8_t)d;
+}
+
+// Token t's key in channel d of an integer record: the word its code is in, and (head: the record's header
+// in LDS) what rounding to fp16 took off it.
+__device__ __forceinline__ int key_entry(int d) { return (d >> 5) << 3 | (d & 7); }  // of a lane's chunk
+__device__ __forceinline__ uint32_t key_code_word(const uint8_t *rec, int level, int t, int d) {
+  const int lane = (t >> 4) * 64 + (d >> 3 & 3) * 16 + (t & 15);
+  return *(const uint32_t *)(rec + kSZBytes + lane * 4 * level + 4 * (key_entry(d) * level >> 5));
+}
+__device__ __forceinline__ uint32_t key_rest(uint32_t w, int level, uint32_t head, int d) {
+  const int kg = d >> 3 & 3, n = key_entry(d);
+  const int pos = level == GKV_INT8   ? 8 * (n & 3)  // code_pos, without tables in memory
+                  : level == GKV_INT4 ? 4 * (1 - (n >> 2 & 1)) + 8 * (n >> 1 & 1) + 16 * (n & 1)
+                                      : (int)(0x20A4C6E8u >> 4 * (n >> 1 & 7) & 15) + 16 * (n & 1);
+  const uint32_t code = w >> pos & ((1u << level) - 1);
+  const uint32_t sc = lds_u16(head + (32 * kg + n) * 2), z = lds_u16(head + 2 * D + (32 * kg + n) * 2);
+  half2v c;
+  c[0] = c[1] = (_Float16)(float)code;
+  const uint32_t y = bounded(decoded(c, sc, z), sc, z) & 0xFFFFu;
+  if ((y & T16::kInf) == T16::kInf) return 0;
+  const float rest = __builtin_fmaf((float)code, (float)halves(sc)[0], (float)halves(z)[0]) - (float)halves(y)[0];
+  return T16::pack(rest, 0.f);
+}
+
+// One workgroup a block or 64 residual rows; a wavefront a page (kRest: tiles with second terms).  Bound by
+// the bytes it writes: 55 us for six sequences of 1343 to 12311 tokens x 8 KV heads (209 MB, 3.8 TB/s).
+template <bool kRest>
 __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
   __shared__ __align__(16) uint8_t sh[1024 + 64];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)sh;
@@ -495,18 +590,19 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
   all = sums[0] + sums[2] + sums[4] + sums[6];
   here = sums[1] + sums[3] + sums[5] + sums[7];
   const ListShape l = list_shape(p, c0, all);
-  uint8_t *list = p.list + (p.list0[s] + (int64_t)h * list_tiles(p, T)) * kListTile;
+  uint8_t *list = p.list + (p.list0[s] + (int64_t)h * list_tiles(p, T)) * p.tile;
   if (v == 0 && tid == 0) p.whole[s * p.Hkv + h] = l.whole;
   const Visit x = visit_at(p, u, v, nblk);
   if (v < c0 && x.level == GKV_MEAN) {  // a row of the one-centroid tiles
     if (pg) return;
-    uint8_t *tile = list + (int64_t)(l.plain + l.res + (here >> 6)) * kListTile;
+    uint8_t *tile = list + (int64_t)(l.plain + l.res + (here >> 6)) * p.tile;
     // the last one's workgroup also writes the places behind it
     const int end = here == l.means - 1 ? ((here >> 6) + 1) * P : here + 1;
     for (int r = here; r < end; ++r) {
       const int t = r & (P - 1), n = r == here ? P - __popcll(x.drop) : 0;
       const u4 none = {0, 0, 0, 0};
       if (lane < 16) *(u4 *)(tile + ta::key_place(t, lane)) = n ? ((const u4 *)x.k)[lane] : none;
+      if (kRest && lane < 2) *(u4 *)(tile + kListTile + (t >> 5) * 1024 + ((t & 31) + 32 * lane) * 16) = none;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int d = lane + 64 * i;
@@ -519,7 +615,7 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
     return;
   }
   const int at = v < c0 ? v - here : v < nblk ? l.whole + v - c0 : l.plain + v - nblk;
-  uint8_t *tile = list + (int64_t)at * kListTile;
+  uint8_t *tile = list + (int64_t)at * p.tile;
   // places without a token: their keys and values are zero, their scores start from -infinity
   uint64_t drop = x.drop;
   if (v >= c0 && v < nblk) drop = 0;  // residual tokens are put in their places
@@ -536,6 +632,16 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
   uint32_t y[16];
   load_raw<GKV_KEYS>(k, x.k, x.level, pg, lane);
   load_raw<GKV_VALUES>(w, x.v, x.level, pg, lane);
+  // hot channels hc .. + 3 of token ht
+  const int ht = tid >> 2, hc = 4 * (tid & 3);
+  uint32_t ids = 0, hw[4] = {0, 0, 0, 0};
+  if (kRest && is_int_level(x.level)) {
+    const int64_t l4 = ((int64_t)s * p.Hkv + h) * (ta::kHot / 4);
+    const uint32_t a = hc & 4 ? table32(p.hot, l4 + 1) : table32(p.hot, l4);
+    ids = hc & 8 ? hc & 4 ? table32(p.hot, l4 + 3) : table32(p.hot, l4 + 2) : a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hw[i] = key_code_word(x.k, x.level, ht, ids >> (8 * i) & 0xFF);
+  }
   const Exponents e;
   key_words_any(y, k, x.level, lds, kg, e);
   if (drop >> (16 * pg + m) & 1)
@@ -544,6 +650,13 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     *(u4 *)(tile + ta::key_place(16 * pg + m, 4 * j + kg)) = u4{y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]};
+  if constexpr (kRest) {
+    u2 rest = {0, 0};
+    if (is_int_level(x.level) && !(x.drop >> ht & 1))
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rest[i >> 1] |= key_rest(hw[i], x.level, lds, ids >> (8 * i) & 0xFF) << (16 * (i & 1));
+    *(u2 *)(tile + kListTile + (ht >> 5) * 1024 + ((ht & 31) + 4 * (hc & 8)) * 16 + 2 * (hc & 7)) = rest;
+  }
   Visit xd = x;
   xd.drop = drop;
   value_words_any(y, w, xd, lds, pg, lane, p.vtok, e);
@@ -590,9 +703,10 @@ __global__ void __launch_bounds__(256) expand_kernel(const ChunkParams p) {
 constexpr int kTileWaves = 8, kTileRows = 32 * kTileWaves;
 
 // A list's tiles: 1 KB a copy.
+template <bool kRest>
 struct ListTiles {
   const uint8_t *list;
-  int wave, lane;
+  int bytes, wave, lane;
   __device__ __forceinline__ void copy(const uint8_t *src, uint32_t lds) const {
 #pragma unroll
     for (int i = 0; i < 16 / kTileWaves; ++i) {
@@ -600,18 +714,23 @@ struct ListTiles {
       ta::dma16(lane * 16, src + at, lds + at);
     }
   }
-  __device__ __forceinline__ void keys(int t, uint32_t lds, uint32_t bias) const {
-    const uint8_t *tile = list + (int64_t)t * kListTile;
+  __device__ __forceinline__ void keys(int t, uint32_t lds, uint32_t bias, uint32_t hot) const {
+    const uint8_t *tile = list + (int64_t)t * bytes;
     copy(tile, lds);
     if (wave == 0 && lane < 16) ta::dma16(lane * 16, tile + 2 * ta::kTileBytes, bias);
+    if (kRest && (wave == 1 || wave == 2)) {
+      const uint32_t at = (wave - 1) * 1024;
+      ta::dma16(lane * 16 + at, tile + kListTile, hot + at);
+    }
   }
   __device__ __forceinline__ void values(int t, uint32_t lds) const {
-    copy(list + (int64_t)t * kListTile + ta::kTileBytes, lds);
+    copy(list + (int64_t)t * bytes + ta::kTileBytes, lds);
   }
 };
 
 // 256 rows over a share of a list, as a prompt's row tile (and as it bound by matrix and vector
 // issue): 512 tokens x 28/4 heads over 64k 476 us (1.0 PFLOP/s).
+template <bool kRest>
 __global__ void __launch_bounds__(64 * kTileWaves, 2) tiles_kernel(const ChunkParams p) {
   extern __shared__ __align__(16) unsigned char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
@@ -628,9 +747,9 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) tiles_kernel(const ChunkPa
   const int ntile = whole + last / P - c0 + 1;
   const int split = p.split[j.s];
   const int t0 = (int)((int64_t)ntile * j.part / split), t1 = (int)((int64_t)ntile * (j.part + 1) / split);
-  const ListTiles src = {p.list + (p.list0[j.s] + (int64_t)j.h * list_tiles(p, j.T)) * kListTile, wave, ln.lane};
+  const ListTiles<kRest> src = {p.list + (p.list0[j.s] + (int64_t)j.h * list_tiles(p, j.T)) * p.tile, p.tile, wave, ln.lane};
   ta::Rows st;
-  u4 q[8];
+  u4 q[kRest ? 9 : 8];
   st.init();
   if (t0 < t1)  // (a row tile with fewer tiles than shares leaves some of them none)
     ta::attend<T16, kTileWaves, false, true>(
@@ -639,7 +758,7 @@ __global__ void __launch_bounds__(64 * kTileWaves, 2) tiles_kernel(const ChunkPa
           const int n = t < whole ? P : j.pos0 + tok + 1 - (c0 + t - whole) * P;
           return n >= P ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
         },
-        [&] { load_queries(q, p, j, tok, g, ln.hf); });
+        [&] { load_queries<kRest>(q, p, j, tok, g, ln.hf); });
   const float l = st.l + ta::other_half(st.l);
   if (row >= j.rows) return;
   if (split == 1)
@@ -809,10 +928,6 @@ __device__ __forceinline__ void few_wait(int level) {
 }
 // LDS reads of what is copied over next have returned.
 __device__ __forceinline__ void few_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-__device__ __forceinline__ uint32_t lds_u16(uint32_t at) {
-  return *(__attribute__((address_space(3))) const uint16_t *)(uintptr_t)at;
-}
 
 // The codes of a lane's chunk of page g.
 template <int BITS>
@@ -1348,12 +1463,14 @@ gkv_status plan_part(Part &t, const gkv_cache *c, int64_t fill) {
 
 struct Plan {
   Part few, many;
-  int64_t part, whole, list, bytes;  // workspace: partials | whole counts | lists
+  bool rest;                               // tiles with second terms
+  int64_t part, whole, hot, list, bytes;  // workspace: partials | whole counts | hot channels | lists
 };
 
 gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
   const int G = c->Hq / c->Hkv;
   pl.few.p.nseq = pl.many.p.nseq = 0;
+  pl.rest = false;
   int64_t rows = 0;
   for (int b = 0; b < c->B; ++b) {
     const int64_t T = seq_tokens(c, b), n = n_new[b];
@@ -1368,6 +1485,14 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
     for (int h = 0; h < c->Hkv && few; ++h)
       for (int64_t i = (T - n) / P; i < (T + P - 1) / P; ++i)
         few &= c->level_host[((int64_t)b * c->Hkv + h) * c->nblk_cap + i] == GKV_EXACT;
+    if (!few && !pl.rest) {
+      const int8_t *lv = c->level_host + (int64_t)b * c->Hkv * c->nblk_cap;
+      for (int h = 0; h < c->Hkv && !pl.rest; ++h, lv += c->nblk_cap) {
+        int8_t bits = 0;  // (a level is its own bit: no exit, so that the loop takes many at once)
+        for (int64_t i = 0; i < (T + P - 1) / P; ++i) bits |= lv[i];
+        pl.rest = bits & (GKV_INT8 | GKV_INT4 | GKV_INT2);
+      }
+    }
     ChunkParams &p = few ? pl.few.p : pl.many.p;
     const int i = p.nseq++;
     p.seq[i] = (uint8_t)b;
@@ -1385,8 +1510,11 @@ gkv_status chunk_plan(const gkv_cache *c, const int32_t *n_new, Plan &pl) {
   auto align = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
   pl.part = 0;
   pl.whole = align((pl.few.part_rows + pl.many.part_rows) * kPart * 4);
-  pl.list = align(pl.whole + (int64_t)pl.many.p.nseq * c->Hkv * 4);
-  pl.bytes = pl.list + pl.many.tiles * kListTile;
+  const int64_t lists = (int64_t)pl.many.p.nseq * c->Hkv;
+  pl.hot = align(pl.whole + lists * 4);
+  pl.list = align(pl.hot + (pl.rest ? lists * ta::kHot : 0));
+  pl.many.p.tile = kListTile + (pl.rest ? ta::kHotBytes : 0);
+  pl.bytes = pl.list + pl.many.tiles * pl.many.p.tile;
   return GKV_OK;
 }
 
@@ -1444,6 +1572,7 @@ extern "C" gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const 
     p.sl2 = 1.4426950408889634f / sqrtf((float)D);
     p.part0 = t == &pl.few ? 0 : pl.few.part_rows;
     p.whole = (int32_t *)((uint8_t *)ws + pl.whole);
+    p.hot = (uint8_t *)ws + pl.hot;
     p.list = (uint8_t *)ws + pl.list;
     const dim3 grid((unsigned)(t->wgs * c->Hkv));
     if (t == &pl.few) {
@@ -1451,8 +1580,17 @@ extern "C" gkv_status gkv_chunk_attn(const uint16_t *q, int64_t q_stride, const 
     } else {
       int most = 0;
       for (int i = 0; i < p.nseq; ++i) most = std::max(most, list_tiles(p.T[i], c->nres));
-      hipLaunchKernelGGL(expand_kernel, dim3(most, c->Hkv, p.nseq), dim3(256), 0, s, p);
-      hipLaunchKernelGGL(tiles_kernel, grid, dim3(64 * kTileWaves), ta::kAttendLds + 2 * ta::kBiasBytes, s, p);
+      const dim3 blocks(most, c->Hkv, p.nseq);
+      const dim3 blk(64 * kTileWaves);
+      const int lds = ta::kAttendLds + 2 * ta::kBiasBytes;
+      if (pl.rest) {
+        hipLaunchKernelGGL(hot_kernel, dim3(c->Hkv, p.nseq), dim3(D), 0, s, p);
+        hipLaunchKernelGGL(expand_kernel<true>, blocks, dim3(256), 0, s, p);
+        hipLaunchKernelGGL(tiles_kernel<true>, grid, blk, lds + 2 * ta::kHotBytes, s, p);
+      } else {
+        hipLaunchKernelGGL(expand_kernel<false>, blocks, dim3(256), 0, s, p);
+        hipLaunchKernelGGL(tiles_kernel<false>, grid, blk, lds, s, p);
+      }
     }
     if (hipGetLastError() != hipSuccess) return GKV_E_HIP;
     if (t->merged) {

@@ -42,7 +42,7 @@ struct PromptTiles {
       ta::dma16((uint32_t)min(r, left) * stride + (u << 4), src, lds + r4 * 256);
     }
   }
-  __device__ __forceinline__ void keys(int t, uint32_t lds, uint32_t) const { copy(t, lds, k, ks, true); }
+  __device__ __forceinline__ void keys(int t, uint32_t lds, uint32_t, uint32_t) const { copy(t, lds, k, ks, true); }
   __device__ __forceinline__ void values(int t, uint32_t lds) const { copy(t, lds, v, vs, false); }
 };
 

@@ -194,14 +194,21 @@ __device__ __forceinline__ void start_scores(f16v (&s)[2], const Lane &ln, uint3
     }
 }
 
+// Key operand of 32-token group t: channels 16 d .. + 15, or (d = 8) the second terms of the tile's
+// hot channels, one unit a lane at `hot`.
+__device__ __forceinline__ u4 key_operand(const Lane &ln, uint32_t kbase, uint32_t hot, int d, int t) {
+  return d < 8 ? lds_u4(kbase + (ln.k0 ^ (d << 5)) + t * 8192) : lds_u4(hot + t * 1024 + ln.lane * 16);
+}
+
 // S^T of a 64-token tile.
-template <class T, bool kBias>
-__device__ __forceinline__ void scores(f16v (&s)[2], const Lane &ln, const u4 (&q)[8], uint32_t kbase, uint32_t bias) {
+template <class T, bool kBias, int NQ>
+__device__ __forceinline__ void scores(f16v (&s)[2], const Lane &ln, const u4 (&q)[NQ], uint32_t kbase, uint32_t bias,
+                                       uint32_t hot) {
   start_scores<kBias>(s, ln, bias);
 #pragma unroll
-  for (int d = 0; d < 8; ++d)
+  for (int d = 0; d < NQ; ++d)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) s[t] = T::mfma(lds_u4(kbase + (ln.k0 ^ (d << 5)) + t * 8192), q[d], s[t]);
+    for (int t = 0; t < 2; ++t) s[t] = T::mfma(key_operand(ln, kbase, hot, d, t), q[d], s[t]);
 }
 
 // Scores of tokens whose bit in vis (of this lane's row) is clear become -infinity.
@@ -340,25 +347,25 @@ __device__ __forceinline__ void add_odd(Rows &r, const u4 &odd) {
 // The value product of one 64-token tile and the key product of the next, one MFMA after the
 // other with the operands read kAhead products before (the order is pinned: left alone, the
 // compiler reads one ahead and every product waits for LDS).
-template <class T, bool kTr, bool kBias>
-__device__ __forceinline__ void multiply(Rows &r, f16v (&s)[2], const Lane &ln, const u4 (&p)[4], const u4 (&q)[8],
-                                         uint32_t vbase, uint32_t kbase, uint32_t bias) {
-  constexpr int kAhead = 6;
+template <class T, bool kTr, bool kBias, int NQ>
+__device__ __forceinline__ void multiply(Rows &r, f16v (&s)[2], const Lane &ln, const u4 (&p)[4], const u4 (&q)[NQ],
+                                         uint32_t vbase, uint32_t kbase, uint32_t bias, uint32_t hot) {
+  constexpr int kAhead = 6, kAll = 16 + 2 * NQ;
   u4 x[kAhead];
   auto operand = [&](int i) {
     if (i < 16) return value_operand<kTr>(ln, vbase, i >> 2, i & 3);
-    return lds_u4(kbase + (ln.k0 ^ (((i - 16) >> 1) << 5)) + (i & 1) * 8192);
+    return key_operand(ln, kbase, hot, (i - 16) >> 1, i & 1);
   };
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) x[i] = operand(i);
   start_scores<kBias>(s, ln, bias);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
+  for (int i = 0; i < kAll; ++i) {
     __builtin_amdgcn_sched_barrier(0);
     const u4 a = x[i % kAhead];
     if (i < 16) r.o[i & 3] = T::mfma(a, p[i >> 2], r.o[i & 3]);
     else s[i & 1] = T::mfma(a, q[(i - 16) >> 1], s[i & 1]);
-    if (i + kAhead < 32) x[i % kAhead] = operand(i + kAhead);
+    if (i + kAhead < kAll) x[i % kAhead] = operand(i + kAhead);
   }
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -389,7 +396,9 @@ __device__ __forceinline__ void store_row(uint16_t *row, const Rows &r, float in
 constexpr int kTile = 64;                  // tokens of a tile
 constexpr int kTileBytes = kTile * 128 * 2;  // of its keys, or of its values
 constexpr int kBiasBytes = kTile * 4;
-constexpr int kAttendLds = 4 * kTileBytes;   // two tiles; with biases 2 kBiasBytes more
+constexpr int kHot = 16;                     // hot channels: those whose keys have second terms
+constexpr int kHotBytes = kTile * kHot * 2;
+constexpr int kAttendLds = 4 * kTileBytes;   // two tiles; biases and second terms: 2 kBiasBytes, 2 kHotBytes more
 
 // LDS copies of 16 bytes a lane, lane after lane from a wave-uniform LDS address.  The compiler puts
 // no wait states in front of inline assembly: the base goes through a scalar move, as a vector
@@ -403,9 +412,9 @@ __device__ __forceinline__ void dma16(uint32_t voff, const void *base, uint32_t 
 }
 
 // The rows of a workgroup over tiles t0 .. t1 - 1 (t0 < t1), those before `full` seen whole by
-// every row; seen(t) gives a lane's row's visible tokens of any other.  src.keys(t, lds)
-// and src.values(t, lds) issue the wavefront's part of a tile's copies.  load() gets the queries, after the first
-// copies are on their way.
+// every row; seen(t) gives a lane's row's visible tokens of any other.  src.keys(t, lds, bias, hot)
+// and src.values(t, lds) issue the wavefront's part of a tile's copies.  load() gets the queries (a ninth operand
+// for the hot channels, where there are any), after the first copies are on their way.
 //
 // The two wavefronts of a SIMD (w and w + WAVES / 2) work half a tile apart: while one
 // multiplies (the last tile's values, this tile's keys) the other forms weights.  In the same
@@ -416,8 +425,8 @@ __device__ __forceinline__ void dma16(uint32_t voff, const void *base, uint32_t 
 // 2 t, the second ones' in 2 t + 1.  Keys t + 1 and values t are copied from the start of
 // interval 2 t on (whose buffers were last read in 2 t - 1; the first ones from the start on) and
 // have arrived at the end of 2 t + 1.
-template <class T, int WAVES, bool kTr, bool kBias, class Src, class Seen, class Load>
-__device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uint32_t lds, int wave, int t0, int t1,
+template <class T, int WAVES, bool kTr, bool kBias, int NQ, class Src, class Seen, class Load>
+__device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[NQ], uint32_t lds, int wave, int t0, int t1,
                                        int full, float sl2, const Src &src, const Seen &seen, const Load &load) {
   const bool second = wave >= WAVES / 2;
   auto keys = [&](int t) { return lds + (t & 1) * kTileBytes; };
@@ -429,7 +438,8 @@ __device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uin
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  auto copy_keys = [&](int t) { src.keys(t, keys(t), bias(t)); };
+  auto hot = [&](int t) { return lds + 4 * kTileBytes + 2 * kBiasBytes + (t & 1) * kHotBytes; };
+  auto copy_keys = [&](int t) { src.keys(t, keys(t), bias(t), hot(t)); };
   auto copy = [&](int t) {
     if (t + 1 < t1) copy_keys(t + 1);
     if (t < t1) src.values(t, values(t));
@@ -450,7 +460,7 @@ __device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uin
   // the queries have arrived (the loop's copies are in flight when they are used: a wait for
   // their loads there would wait for the copies)
 #pragma unroll
-  for (int d = 0; d < 8; ++d) asm volatile("" : "+v"(q[d]));
+  for (int d = 0; d < NQ; ++d) asm volatile("" : "+v"(q[d]));
   st.init();
   f16v s[2];
   u4 pr[4];
@@ -458,13 +468,13 @@ __device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uin
   arrived();
   meet();
   if (second) meet();
-  scores<T, kBias>(s, ln, q, keys(t0), bias(t0));
+  scores<T, kBias>(s, ln, q, keys(t0), bias(t0), hot(t0));
   after(t0 - 1);
   int t = t0;
   for (; t < full; ++t) {
     weights<T, 2>(pr, st, s, sl2);
     before(t);
-    multiply<T, kTr, kBias>(st, s, ln, pr, q, values(t), keys(t + 1), bias(t + 1));
+    multiply<T, kTr, kBias>(st, s, ln, pr, q, values(t), keys(t + 1), bias(t + 1), hot(t + 1));
     after(t);
   }
   u4 odd = {0, 0, 0, 0};  // infinities and NaN among the values from here on
@@ -476,7 +486,7 @@ __device__ __forceinline__ void attend(Rows &st, const Lane &ln, u4 (&q)[8], uin
     const bool clean = find_odd<T, 2, kTr>(ln, values(t), vis, odd);
     outputs_clean<T, 2, kTr>(st, ln, pr, values(t), clean);
     if (t == t1 - 1) break;
-    scores<T, kBias>(s, ln, q, keys(t + 1), bias(t + 1));
+    scores<T, kBias>(s, ln, q, keys(t + 1), bias(t + 1), hot(t + 1));
     after(t);
   }
   if (!second) meet();
