@@ -865,9 +865,9 @@ __device__ __forceinline__ void few_weights(uint32_t (&p)[8], FewRows &r, const 
   if (__builtin_expect(__any(top > r.raise), 0)) {
     const float high = over_groups(top);
     const bool mine = high > r.raise;
-    const float up = mine ? high - ta::kLead : 0.f;
+    const float up = mine ? high - T16::kLead : 0.f;
     const float f = r.raise < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
-    r.raise = mine ? ta::kRescale : r.raise;
+    r.raise = mine ? T16::kRescale : r.raise;
     r.m += up;
     r.l *= f;
 #pragma unroll

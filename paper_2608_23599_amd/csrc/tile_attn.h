@@ -17,15 +17,16 @@
 // same order: the probabilities never leave their lane.  O^T has a row per lane too, so the
 // rescale by a moved reference is one factor per lane.
 //
-// Weights are taken relative to a reference that is set kLead (2^7) below the largest score so
-// far and only moved when a score passes it by more than kRescale (2^15): the largest weight of a
-// row lies between 2^7 and 2^15, the sums are in fp32 and the common tile has no cross-lane step.
-// So fp16 weights use the type's range on both sides: they stay below its 65504, are normal
+// Weights are taken relative to a reference that is set kLead (log2 units) below the largest score so
+// far and only moved when a score passes it by more than kRescale, 8 further: the sums are in fp32 and the
+// common tile has no cross-lane step.  In fp16 (7 and 15) the largest weight of a row lies between 2^7 and
+// 2^15, so that weights use the type's range on both sides: they stay below its 65504, are normal
 // numbers down to 2^-21 of the largest one and vanish below 2^-32 of it.  (With the reference at
 // the largest score itself they vanished below 2^-25: beside one token that took nearly all of a
-// row's weight, 16384 others of together 5e-4 were lost.)  Weights enter the second product
-// in the type of the values (one rounding of at most half a step each); the sum of a row adds
-// the rounded ones, so the weights of a row sum to 1 as the product sees them.
+// row's weight, 16384 others of together 5e-4 were lost.)  In bf16, which has fp32's range, the reference is
+// the largest score (7 below, 16k tokens x 28/4 heads took 1844 us instead of 1820).  Weights enter the
+// second product in the type of the values (one rounding of at most half a step each); the sum of a row
+// adds the rounded ones, so the weights of a row sum to 1 as the product sees them.
 //
 // A masked score becomes -infinity by selection, never by arithmetic, so a NaN or infinity
 // in a masked key has no effect; for masked values see find_odd.
@@ -48,10 +49,9 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
-constexpr float kRescale = 15.0f;  // an exponent above this moves the reference (log2 units)
-constexpr float kLead = 7.0f;      // the largest one's exponent when it has moved
-
 struct F16 {
+  static constexpr float kRescale = 15.0f;  // an exponent above this moves the reference
+  static constexpr float kLead = 7.0f;      // the largest one's exponent when it has moved
   static constexpr uint32_t kInf = 0x7C00u, kExp = 0x7C007C00u;  // infinity; the exponent bits of a pair
   __device__ static f16v mfma(u4 a, u4 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0,
@@ -77,6 +77,7 @@ struct F16 {
   }
 };
 struct BF16 {
+  static constexpr float kRescale = 8.0f, kLead = 0.0f;
   static constexpr uint32_t kInf = 0x7F80u, kExp = 0x7F807F80u;
   __device__ static f16v mfma(u4 a, u4 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
@@ -240,9 +241,9 @@ __device__ __forceinline__ void weights(u4 (&p)[2 * NT], Rows &r, const f16v (&s
     // so that a row's rounding does not depend on its neighbours'
     const float high = fmaxf(top, other_half(top));
     const bool go = high > r.raise;
-    const float up = go ? high - kLead : 0.f;
+    const float up = go ? high - T::kLead : 0.f;
     const float f = r.raise < 0.f ? 0.f : __builtin_amdgcn_exp2f(-up);
-    r.raise = go ? kRescale : r.raise;
+    r.raise = go ? T::kRescale : r.raise;
     r.m += up;
     r.l *= f;
 #pragma unroll
