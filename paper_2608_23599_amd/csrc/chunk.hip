@@ -729,7 +729,8 @@ struct ListTiles {
 };
 
 // 256 rows over a share of a list, as a prompt's row tile (and as it bound by matrix and vector
-// issue): 512 tokens x 28/4 heads over 64k 476 us (1.0 PFLOP/s).
+// issue): 512 tokens x 28/4 heads over 64k 515 us with second terms (0.93 PFLOP/s without counting them) and
+// 476 without.
 template <bool kRest>
 __global__ void __launch_bounds__(64 * kTileWaves, 2) tiles_kernel(const ChunkParams p) {
   extern __shared__ __align__(16) unsigned char smem[];

@@ -50,7 +50,7 @@ struct PromptTiles {
 // wavefronts a SIMD, in one workgroup or two (see launch).  Bound by matrix and vector issue beside one another (1.87 us
 // for 256 rows x 64 tokens), and in short prompts by the first copies, masked tiles and stores, about
 // 6 us a workgroup of eight wavefronts with nothing else on its unit.  28/4 heads in bf16: one prompt of 16k tokens
-// 1770 us (1.09 PFLOP/s; a large library product reaches 1.27), sixteen of 107 to 2000 210 to 226;
+// 1770 to 1840 us from card to card (1.05 to 1.09 PFLOP/s; a large library product reaches 1.27), sixteen of 107 to 2000 210 to 226;
 // 32/8 heads in fp16, 4k tokens: 146 us.
 template <class T, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(const PromptParams p) {
