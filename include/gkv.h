@@ -470,7 +470,7 @@ gkv_status gkv_truncate(gkv_cache *c, gkv_pool *pool, const int64_t *koff_host, 
  * (GKV_E_SHAPE) and 0 for a retired one (GKV_E_ARG).  Lengths and levels are those of the
  * host mirrors at the call; a captured call replays for them.
  * ws: gkv_chunk_ws_bytes(c, n_new_host) bytes (16-byte aligned, no initialisation; may be
- * NULL when that is 0), which depends on the lengths and on the current device's compute units
+ * NULL when that is 0), which depends on the lengths, levels and the current device's compute units
  * (-1: the call would be refused).  Where more than 128 rows of a sequence attend (or a block that one
  * sees in part is not exact) it holds the sequence's cache decoded, 33024 bytes for every block
  * and every 64 residual rows of a KV head (35072 if one of them is an integer block).
