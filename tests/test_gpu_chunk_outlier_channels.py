@@ -80,3 +80,26 @@ def test_few_integer_blocks(gpu, places):
     codes = np.repeat(levels == 8, 64)[:T]
     o, bound = rows_and_bounds(q[:, 0].astype(np.float64), kh, vh, codes, codes)
     assert (np.linalg.norm(out[:, 0] - o, axis=1) / bound).max() <= 1.0
+
+
+@pytest.mark.gpu
+def test_captured_calls(gpu):
+    """Two captured calls of many rows, replayed with new queries between eager calls of the same cache."""
+    import torch
+    ks, vs, q = data(11, 2, 4)
+    cache = gpu.GradedCache.build(ks, vs, Hq=2, levels=np.array([2] * 20 + [4] * 30 + [8] * 27 + [16] * 4, np.int8))
+    q = torch.from_numpy(q).cuda()
+    outs, graphs = [torch.empty_like(q) for _ in range(2)], []
+    cache.chunk_attn(q, [N])
+    for out in outs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            cache.chunk_attn(q, [N], out=out)
+    for _ in range(4):
+        q.copy_(torch.roll(q, 1, 0))
+        for g, out in zip(graphs, outs):
+            out.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        want = cache.chunk_attn(q, [N])
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
